@@ -319,7 +319,7 @@ def _plain_verify(s):
                     (w - _fixed(qd[rows, n.clamp(max=K - 1)])).clamp(min=0), w)
     cum = w.cumsum(1)
     total = cum[:, -1]
-    r = (u[rows, n].double() * 2.0 ** 24).long()
+    r = (u[:, K].double() * 2.0 ** 24).long()  # the number that no draft was judged by
     t = (total >> 24) * r + ((total & 0xffffff) * r >> 24)
     nxt = torch.where(total > 0, (cum <= t[:, None]).sum(1), -1)
     col = torch.arange(K + 1, device="cuda")
@@ -457,7 +457,7 @@ def _exact_verify(case, s):
         w = np.floor(p[b, i] * 2.0 ** 40).astype(np.int64)
         if i < lens[b]:
             w = np.maximum(w - np.floor(qd[b, i] * 2.0 ** 40).astype(np.int64), 0)
-        total, r = int(w.sum()), int(u[b, i] * 2 ** 24)
+        total, r = int(w.sum()), int(u[b, K] * 2 ** 24)
         accepted[b] = i
         if total:
             out[b, i] = int(np.searchsorted(np.cumsum(w), total * r >> 24, side="right"))
