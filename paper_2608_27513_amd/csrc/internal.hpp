@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "damp.h"
+#include "damp_serving.h"
 
 namespace damp {
 
@@ -61,6 +62,17 @@ damp_status check_pool(const damp_pool* pool);
 // with DAMP_ERR_INVALID_ARG if a slot inside the pool occurs twice. Without
 // it: DAMP_OK at once. Called by every entry point that writes tiles.
 damp_status debug_check_slots(const damp_pool* pool, const int32_t* slot_idx, int32_t B,
+                              hipStream_t stream, const char* name);
+
+// Whether DAMP_CHECK_SLOTS asks for the checks of slot ids.
+bool slots_checked();
+
+// The check of a call that reads the n slots of one device list and writes the
+// m of another: fails with DAMP_ERR_INVALID_ARG if a slot of the pool is in
+// both, except, with `in_place`, at the same place of both. Synchronises
+// `stream`.
+damp_status check_slots_apart(const damp_pool* pool, const int32_t* read, int32_t n,
+                              const int32_t* written, int32_t m, bool in_place,
                               hipStream_t stream, const char* name);
 
 // Thread-local error message.

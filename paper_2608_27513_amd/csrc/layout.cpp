@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "internal.hpp"
@@ -202,9 +203,38 @@ damp_status check_slots(const damp_pool* pool, const int32_t* slot_idx, int32_t 
 
 damp_status debug_check_slots(const damp_pool* pool, const int32_t* slot_idx, int32_t B,
                               hipStream_t stream, const char* name) {
-  const char* env = std::getenv("DAMP_CHECK_SLOTS");
-  if (!env || env[0] == '\0' || env[0] == '0') return DAMP_OK;
+  if (!slots_checked()) return DAMP_OK;
   return check_slots(pool, slot_idx, B, true, stream, name);
+}
+
+damp_status check_slots_apart(const damp_pool* pool, const int32_t* read, int32_t n,
+                              const int32_t* written, int32_t m, bool in_place,
+                              hipStream_t stream, const char* name) {
+  std::vector<int32_t> from(static_cast<size_t>(n)), to(static_cast<size_t>(m));
+  hipError_t e = hipMemcpyAsync(from.data(), read, sizeof(int32_t) * from.size(),
+                                hipMemcpyDeviceToHost, stream);
+  if (e == hipSuccess)
+    e = hipMemcpyAsync(to.data(), written, sizeof(int32_t) * to.size(), hipMemcpyDeviceToHost,
+                       stream);
+  if (e == hipSuccess) e = hipStreamSynchronize(stream);
+  if (e != hipSuccess) return fail(DAMP_ERR_HIP, "%s: slot ids: %s", name, hipGetErrorString(e));
+  std::vector<std::pair<int32_t, int32_t>> readers;  // (slot, entry)
+  for (int32_t i = 0; i < n; ++i) readers.emplace_back(from[i], i);
+  std::sort(readers.begin(), readers.end());
+  for (int32_t j = 0; j < m; ++j) {
+    if (to[j] < 0 || to[j] >= pool->num_slots) continue;
+    for (auto r = std::lower_bound(readers.begin(), readers.end(), std::make_pair(to[j], 0));
+         r != readers.end() && r->first == to[j]; ++r)
+      if (!in_place || r->second != j)
+        return fail(DAMP_ERR_INVALID_ARG, "%s: slot %d is written for entry %d and read for %d",
+                    name, to[j], j, r->second);
+  }
+  return DAMP_OK;
+}
+
+bool slots_checked() {
+  const char* env = std::getenv("DAMP_CHECK_SLOTS");
+  return env && env[0] != '\0' && env[0] != '0';
 }
 
 }  // namespace damp

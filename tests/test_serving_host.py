@@ -1,0 +1,183 @@
+"""Host-side checks of the serving operators: exports, workspace sizes and
+refusals. No GPU needed: every call fails validation or has nothing to do."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import serving_ref as ref
+from paper_2608_27513_amd import damp as D
+from paper_2608_27513_amd import serving as S
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "damp_serving.h")
+P = ctypes.c_void_p(0x7f0000100000)  # never dereferenced
+ODD = ctypes.c_void_p(0x7f0000100008)
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(D.LIB_PATH):
+        from paper_2608_27513_amd import build
+        build.build()
+    return S.lib()
+
+
+def pool_of(dk=64, dv=64, kind=D.DAMP_STATE_FP32, layers=2, slots=4, hv=8):
+    lay = D.damp_layout_init(dk, dv, 0, kind)
+    pool = D.damp_pool()
+    need = D.damp_pool_required_bytes(lay, layers, slots, hv)
+    assert D.lib().damp_pool_init(ctypes.byref(pool), ctypes.byref(lay), layers, slots, hv,
+                                  ctypes.c_void_p(0x7f0000000000), need) == 0
+    return pool
+
+
+def status(fn, *args):
+    return fn(*args), D.lib().damp_last_error().decode()
+
+
+def test_every_declared_symbol_is_exported(L):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(damp_[a-z0-9_]+)\s*\(", text)))
+    assert names == sorted(S.EXPORTS)
+    for n in names:
+        assert hasattr(L, n), n
+
+
+# the arguments num_k_heads .. o_dtype of both linear-attention calls
+OPERANDS = [4, P, 256, P, 256, P, 512, P, 8, 1.0, P, D.DAMP_DT_FP32]
+BAD_OPERANDS = {"num_k_heads 3": (0, 3), "num_k_heads 0": (0, 0), "q": (1, None), "q odd": (1, ODD),
+                "q_stride short": (2, 248), "q_stride odd": (2, 260), "k": (3, None),
+                "k odd": (3, ODD), "k_stride 0": (4, 0), "v": (5, None), "v odd": (5, ODD),
+                "v_stride": (6, 504), "v_stride negative": (6, -512), "g": (7, None),
+                "g_stride 4": (8, 4), "g_stride negative": (8, -8), "o": (10, None),
+                "o odd": (10, ODD), "o_dtype": (11, D.DAMP_DT_FP16), "q far": (2, 2 ** 62)}
+
+
+@pytest.mark.parametrize("what", BAD_OPERANDS)
+def test_linear_operands(L, what):
+    pool = pool_of()
+    args = list(OPERANDS)
+    i, args[i] = BAD_OPERANDS[what]
+    for st, msg in (status(L.damp_linear_update, ctypes.byref(pool), 0, P, P, 3, *args, None),
+                    status(L.damp_linear_prefill, ctypes.byref(pool), 0, P, P, 3, 100, 50, P, P,
+                           *args, P, 1 << 40, None)):
+        assert st == D.DAMP_ERR_INVALID_ARG and msg
+
+
+def test_linear_refusals(L):
+    pool = pool_of()
+    up = [ctypes.byref(pool), 0, P, None, 3, *OPERANDS, None]
+    for i, val in ((0, None), (1, 2), (1, -1), (2, None), (4, -1), (4, 65536)):
+        a = list(up)
+        a[i] = val
+        assert L.damp_linear_update(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+    a = list(up)
+    a[4] = 0
+    assert L.damp_linear_update(*a) == D.DAMP_OK
+    pre = [ctypes.byref(pool), 0, P, None, 3, 100, 50, P, P, *OPERANDS, P, 1 << 40, None]
+    for i, val in ((0, None), (1, 2), (2, None), (4, -1), (5, -1), (5, 2 ** 31), (6, -1), (6, 101),
+                   (7, None), (8, None)):
+        a = list(pre)
+        a[i] = val
+        assert L.damp_linear_prefill(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+    a = list(pre)
+    a[4] = 0
+    assert L.damp_linear_prefill(*a) == D.DAMP_OK
+    for bad in (pool_of(kind=D.DAMP_STATE_MIXED), pool_of(dk=60), pool_of(dv=264), pool_of(dv=4)):
+        st, msg = status(L.damp_linear_update, ctypes.byref(bad), *up[1:])
+        assert st == D.DAMP_ERR_UNSUPPORTED and "multiples of 8" in msg
+        st, _ = status(L.damp_linear_prefill, ctypes.byref(bad), *pre[1:])
+        assert st == D.DAMP_ERR_UNSUPPORTED
+
+
+def test_verify_refusals(L):
+    need = L.damp_verify_workspace_bytes(4, 1000)
+    assert need > 0
+    for B, V in ((0, 10), (-1, 10), (65536, 10), (4, 0), (4, 2 ** 22 + 1)):
+        assert L.damp_verify_workspace_bytes(B, V) == 0
+    args = [P, P, D.DAMP_DT_FP32, P, None, P, 4, 3, 1000, P, P, P, need, None]
+    for i, val in ((0, None), (1, None), (2, D.DAMP_DT_FP16), (3, None), (5, None), (6, -1),
+                   (6, 65536), (7, -1), (7, 1025), (8, 0), (8, 2 ** 22 + 1), (9, None), (10, None),
+                   (11, None), (11, ODD), (12, need - 1)):
+        a = list(args)
+        a[i] = val
+        st, msg = status(L.damp_verify_drafts, *a)
+        assert st == D.DAMP_ERR_INVALID_ARG and msg, (i, val)
+    a = list(args)
+    a[6] = 0
+    assert L.damp_verify_drafts(*a) == D.DAMP_OK
+
+
+def test_slots_refusals(L):
+    for fn in (L.damp_slots_alloc, L.damp_slots_retain, L.damp_slots_release):
+        for args in ((P, 0, P, 3), (P, -1, P, 3), (None, 8, P, 3), (P, 8, None, 3), (P, 8, P, -1)):
+            assert fn(*args, None) == D.DAMP_ERR_INVALID_ARG
+        assert fn(P, 8, P, 0, None) == D.DAMP_OK
+    pool = ctypes.byref(pool_of())
+    fork = [pool, -1, P, P, 3, 2, None]
+    for i, val in ((0, None), (1, -2), (1, 2), (2, None), (3, None), (4, -1), (5, -1), (4, 2 ** 30)):
+        a = list(fork)
+        a[i] = val
+        a[5] = 4 if (i, val) == (4, 2 ** 30) else a[5]
+        assert L.damp_slots_fork(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+    for i in (4, 5):
+        a = list(fork)
+        a[i] = 0
+        assert L.damp_slots_fork(*a) == D.DAMP_OK
+    need = L.damp_slots_compact_workspace_bytes(pool)
+    assert need >= 2 * 4 * 4 and L.damp_slots_compact_workspace_bytes(None) == 0
+    comp = [pool, P, P, P, P, need, None]
+    for i, val in ((0, None), (1, None), (2, None), (3, None), (4, None), (4, ODD), (5, need - 1)):
+        a = list(comp)
+        a[i] = val
+        assert L.damp_slots_compact(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+
+
+# ----------------------------------------- the plain implementations themselves
+
+def test_reference_recurrence_against_the_sum_over_tokens():
+    """o_t = scale sum_j exp(g_{j+1} + .. + g_t) (q_t . k_j) v_j, from a zero state."""
+    gen = torch.Generator().manual_seed(0)
+    T, HV, HK, dk, dv = 9, 4, 2, 5, 3
+    q, k = (torch.randn(T, HK, dk, generator=gen) for _ in range(2))
+    v, g = torch.randn(T, HV, dv, generator=gen), -torch.rand(T, HV, generator=gen)
+    o, _ = ref.linear(q, k, v, g, torch.zeros(HV, dk, dv), 0.5)
+    for t in range(T):
+        for h in range(HV):
+            want = sum(float(torch.exp(g[j + 1:t + 1, h].double().sum()))
+                       * float(q[t, h // 2].double() @ k[j, h // 2].double()) * v[j, h].double()
+                       for j in range(t + 1)) * 0.5
+            assert torch.allclose(o[t, h], want, rtol=1e-12)
+
+
+def test_reference_verification_distributes_as_the_target():
+    """Over many uniform numbers the first token follows p whatever q is."""
+    rng = np.random.RandomState(1)
+    V, n = 6, 40000
+    p0 = np.array([0.3, 0.05, 0.25, 0.1, 0.2, 0.1])
+    q0 = np.array([0.1, 0.3, 0.1, 0.1, 0.3, 0.1])
+    p = np.broadcast_to(np.stack([p0, p0]), (n, 2, V))
+    q = np.broadcast_to(q0, (n, 1, V))
+    tokens = rng.choice(V, size=(n, 1), p=q0)
+    u = rng.randint(0, 1 << 24, (n, 2)) / 2.0 ** 24
+    a, out = ref.verify(p, q, tokens, u, np.ones(n, int))
+    kept = a == 1
+    assert np.abs(np.bincount(out[:, 0], minlength=V) / n - p0).max() <= 5 / np.sqrt(n)
+    assert np.abs(np.bincount(out[kept, 1], minlength=V) / kept.sum() - p0).max() <= 5 / np.sqrt(n)
+    assert abs(kept.mean() - np.minimum(p0, q0).sum()) <= 5 / np.sqrt(n)
+
+
+def test_reference_compaction_keeps_every_live_slot():
+    rng = np.random.RandomState(2)
+    for _ in range(50):
+        refs = rng.randint(0, 3, rng.randint(1, 30))
+        where, new, live, moves = ref.compact(refs)
+        assert sorted(where[where >= 0]) == list(range(live))
+        assert (new[live:] == 0).all() and (new[:live] > 0).all()
+        assert len(moves) == int((refs[:live] == 0).sum())
+        for s in range(len(refs)):
+            assert refs[s] == 0 or new[where[s]] == refs[s]
