@@ -1,16 +1,63 @@
-// Linear attention with one decay a head over packed prompts.
+// Linear attention with one decay a head over packed prompts, on the matrix
+// cores.
+//
+// A request's tokens are taken in chunks of C = 64. With L_i the sum of the
+// log-decays of a chunk's tokens up to i, and S the state before it,
+//   o_i = scale (exp(L_i) S^T q_i + sum_{j <= i} exp(L_i - L_j) (q_i . k_j) v_j)
+//   S'  = exp(L_C) S + sum_j k_j (exp(L_C - L_j) v_j)^T
+// which are four products: K Q^T, S^T Q^T, V^T P^T (P the decayed, causal
+// scores) and K^T (D V).
+//
+// A workgroup owns up to 128 columns of the state of one (request, value
+// head), 32 columns a wave, in accumulators for its whole run of tokens. All
+// products are 32x32x16 bf16 instructions, whose results hold column n of a
+// lane in the order that the next product wants its operand: with
+//   k slots (lane half h, j = 0 .. 7)  <->  rows 16 s + 4 h + j (+ 4 if j > 3)
+// the state's accumulators are S^T's operand and the scores' are P^T's without
+// leaving the lane. Q and K are stored in LDS with the middle two quads of
+// every 16 channels swapped, so that these 8 rows are 16 neighbouring bytes;
+// K^T and V^T come through transposing LDS reads.
+//
+// q, k, v are bf16 and enter as they are. What is fp32 (S, P, D V) enters as
+// a sum of bf16 parts, x = x1 + x2 (+ x3), each the rounding of what the
+// parts before it leave: three parts hold all 24 bits (the state, and o in
+// fp32), two hold 16 (for o in bf16, whose own rounding is 2^-8).
+//
+// Log-decays are summed in double, in units of log2: their differences stay
+// good to fp32 however far the sum has run. A log-decay below -1000 counts as
+// that (its factor is 0 in fp32 either way), so -inf makes no inf - inf.
+//
+// Where there are fewer requests and heads than the device has room for, the
+// tokens are cut into segments: a first pass leaves the state that each
+// segment adds, a second runs over the segments to the state before each,
+// and the third works on all segments at once.
+#include <algorithm>
+
 #include "device.hpp"
 #include "linear.hpp"
 
 namespace damp {
 namespace {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kChunk = 64;
+constexpr float kLeastLog = -1000.0f;
+constexpr double kLog2e = 1.4426950408889634;
+
 struct PromptParams {
   LinearParams l;
   const int32_t* seq_start;
   const int32_t* seq_len;
+  float* seg_states;  // [B, segments, HV, dk, dv]
+  float* seg_decays;  // [B, segments, HV]
   int32_t n_tokens;
   int32_t max_len;
+  int32_t seg_len;   // tokens, a multiple of kChunk
+  int32_t segments;  // of the longest request
 };
 
 // First token and length of request b, within the token axis and max_len.
@@ -22,83 +69,428 @@ __device__ __forceinline__ void request_range(const PromptParams& p, int b, int&
   if (!inside) start = 0;
 }
 
-// The recurrence token by token: a workgroup owns 32 columns of one (request,
-// value head) state in registers, 8 lanes a row.
-__global__ __launch_bounds__(256) void prompt_recurrent(const PromptParams pp) {
+__device__ __forceinline__ int segments_of(const PromptParams& p, int len) {
+  return len > 0 ? (len - 1) / p.seg_len + 1 : 1;
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Eight values as PARTS bf16 vectors that add up to them.
+template <int PARTS>
+__device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&out)[PARTS]) {
+#pragma unroll
+  for (int n = 0; n < PARTS; ++n) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+      if (n + 1 < PARTS) {
+        x[2 * j] -= bf16_lo(w[j]);
+        x[2 * j + 1] -= bf16_hi(w[j]);
+      }
+    }
+    out[n] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Four tokens of one column per lane, from rows of 16-bit values in LDS: each
+// lane gives the place of four columns of one token.
+__device__ __forceinline__ uint2 read_columns(const uint16_t* at) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at));
+}
+__device__ __forceinline__ bf16x8 read_columns8(const uint16_t* at, int step) {
+  const uint2 a = read_columns(at), b = read_columns(at + step);
+  const u32x4 w = {a.x, a.y, b.x, b.y};
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// PARTS = 0: the first pass, which leaves the state of each segment but the
+// last from a zero start. PARTS = 2 or 3: outputs, with so many parts of S
+// and P.
+template <int DK, int NW, int PARTS>
+__global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) {
   const LinearParams& p = pp.l;
-  __shared__ float red[2][4][32];
-  const int t = threadIdx.x;
-  const int h = blockIdx.x, b = blockIdx.y;
-  const int cg = t % 8, rg = t / 8;
-  const int col = blockIdx.z * 32 + 4 * cg;
-  const bool in_row = col < p.dv;
+  constexpr bool kOut = PARTS > 0;
+  constexpr int NT = 64 * NW;
+  constexpr int KT = DK / 32;             // state tiles of a wave
+  constexpr int QS = DK + 8;              // row of Q in LDS, 16-bit values
+  constexpr int KS = DK + 32, VS = 32 * NW + 32;
+  constexpr int KV = 64 * (DK / 8) / NT;  // 16-byte loads of a thread for K (and Q)
+  constexpr int VV = 4;                   // and for V
+  constexpr int NP = kOut ? PARTS : 1;
+
+  __shared__ __attribute__((aligned(16))) uint16_t kt[kChunk * KS];
+  __shared__ __attribute__((aligned(16))) uint16_t qt[kOut ? kChunk * QS : 8];
+  __shared__ __attribute__((aligned(16))) uint16_t vt[kChunk * VS];
+  __shared__ u32x4 pt[kOut ? 3 * 2 * NP * 64 : 1];
+  __shared__ double logs[kChunk];
+  __shared__ float to_end[kChunk], from_start[kChunk];
+
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int half = lane >> 5, n32 = lane & 31;
+  const int blocks_v = (p.dv + 32 * NW - 1) / (32 * NW);
+  const int nx = p.HV * blocks_v;
+  // heads that share keys on one XCD (workgroups go to the 8 XCDs in turn)
+  const int x = nx % 8 == 0 ? (blockIdx.x % 8) * (nx / 8) + blockIdx.x / 8 : blockIdx.x;
+  const int h = x / blocks_v, col0 = (x % blocks_v) * 32 * NW;
+  const int b = blockIdx.y, seg = blockIdx.z;
   const int hk = h / (p.HV / p.HK);
+
+  int start, len;
+  request_range(pp, b, start, len);
+  const int segs = segments_of(pp, len);
+  if (seg >= (kOut ? segs : segs - 1)) return;
+  const int64_t tok0 = static_cast<int64_t>(start) + static_cast<int64_t>(seg) * pp.seg_len;
+  const int count = min(pp.seg_len, len - seg * pp.seg_len);
+
   const int from = p.slot_in[b], to = p.slot_out[b];
   const bool old = from >= 0 && from < p.num_slots;
   const bool keep = to >= 0 && to < p.num_slots;
-  const bool padded = !old && from != DAMP_SLOT_ZERO;
-  int start, len;
-  request_range(pp, b, start, len);
-
-  const float* src = reinterpret_cast<const float*>(
-      p.layer_base + (old ? from : 0) * p.slot_stride + h * p.tile_stride);
-  float x[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = rg + 32 * i;
-    float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (old && in_row && r < p.dk)
-      w = *reinterpret_cast<const float4*>(src + static_cast<size_t>(r) * p.dv + col);
-    x[i][0] = w.x;
-    x[i][1] = w.y;
-    x[i][2] = w.z;
-    x[i][3] = w.w;
+  if (!old && from != DAMP_SLOT_ZERO) {  // padded request
+    if constexpr (kOut) {
+      const int w = min(p.dv - col0, 32 * NW);
+      for (int64_t i = t; i < static_cast<int64_t>(count) * w; i += NT) {
+        const size_t at = (static_cast<size_t>(tok0 + i / w) * p.HV + h) * p.dv + col0 + i % w;
+        if (p.o_bf16) static_cast<uint16_t*>(p.o)[at] = 0;
+        else static_cast<float*>(p.o)[at] = 0.0f;
+      }
+    }
+    return;
   }
-  for (int tok = 0; tok < len; ++tok) {
-    const int64_t at = static_cast<int64_t>(start) + tok;
-    const float a = expf(p.g[at * p.g_stride + h]);
-    float vv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (in_row)
+
+  const uint16_t* kb = p.k + hk * p.dk;
+  const uint16_t* qb = p.q + hk * p.dk;
+  const uint16_t* vb = p.v + static_cast<int64_t>(h) * p.dv + col0;
+  const float* gb = p.g + h;
+
+  // ---- the state before the first token
+  const int col = col0 + 32 * wave + n32;
+  const size_t tile = (static_cast<size_t>(b) * pp.segments * p.HV + h) * p.dk * p.dv;
+  const size_t tile_step = static_cast<size_t>(p.HV) * p.dk * p.dv;
+  f32x16 S[KT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) vv[j] = bf16_to_f32(p.v[at * p.v_stride + h * p.dv + col + j]);
+  for (int c = 0; c < KT; ++c)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = rg + 32 * i;
-      if (r >= p.dk) break;
-      const float kr = bf16_to_f32(p.k[at * p.k_stride + hk * p.dk + r]);
-      const float qr = bf16_to_f32(p.q[at * p.q_stride + hk * p.dk + r]);
+    for (int r = 0; r < 16; ++r) S[c][r] = 0.0f;
+  if constexpr (kOut) {
+    const float* src = nullptr;
+    if (segs > 1)
+      src = pp.seg_states + tile + seg * tile_step;
+    else if (old)
+      src = reinterpret_cast<const float*>(p.layer_base + from * p.slot_stride + h * p.tile_stride);
+    if (src && col < p.dv) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[i][j] = fmaf(kr, vv[j], a * x[i][j]);
-        acc[j] = fmaf(qr, x[i][j], acc[j]);
+      for (int c = 0; c < KT; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
+          if (row < p.dk) S[c][r] = src[static_cast<size_t>(row) * p.dv + col];
+        }
+    }
+  }
+
+  // ---- loads of a chunk: rows past the end and columns past the head are zero
+  uint4 kr[KV], qr[kOut ? KV : 1], vr[VV];
+  float gr = 0.0f;
+  auto load = [&](int first) {
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+      const int e = t + NT * i, row = e / (DK / 8), c8 = 8 * (e % (DK / 8));
+      const bool in = first + row < count && c8 < p.dk;
+      const int64_t tok = tok0 + first + row;
+      kr[i] = zero;
+      if (in) kr[i] = *reinterpret_cast<const uint4*>(kb + tok * p.k_stride + c8);
+      if constexpr (kOut) {
+        qr[i] = zero;
+        if (in) qr[i] = *reinterpret_cast<const uint4*>(qb + tok * p.q_stride + c8);
       }
     }
 #pragma unroll
-    for (int m = 8; m < 64; m <<= 1)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], m, 64);
-    if ((t & 63) < 8)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) red[tok & 1][t >> 6][4 * cg + j] = acc[j];
+    for (int i = 0; i < VV; ++i) {
+      const int e = t + NT * i, row = e / (4 * NW), c8 = 8 * (e % (4 * NW));
+      const bool in = first + row < count && col0 + c8 < p.dv;
+      vr[i] = zero;
+      if (in)
+        vr[i] = *reinterpret_cast<const uint4*>(vb + (tok0 + first + row) * p.v_stride + c8);
+    }
+    if (t < kChunk) gr = first + t < count ? gb[(tok0 + first + t) * p.g_stride] : 0.0f;
+  };
+
+  double run_log = 0.0;  // of the segment so far, in the first wave
+  if (count > 0) load(0);
+  for (int first = 0; first < count; first += kChunk) {
     __syncthreads();
-    const int c = blockIdx.z * 32 + t;
-    if (t < 32 && c < p.dv) {
-      const float(&w)[4][32] = red[tok & 1];
-      const float o = padded ? 0.0f : p.scale * ((w[0][t] + w[1][t]) + (w[2][t] + w[3][t]));
-      const size_t o_at = (static_cast<size_t>(at) * p.HV + h) * p.dv + c;
-      if (p.o_bf16) static_cast<uint16_t*>(p.o)[o_at] = f32_to_bf16(o);
-      else static_cast<float*>(p.o)[o_at] = o;
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+      // quads 0 1 2 3 of 16 channels are stored as 0 2 1 3
+      const int e = t + NT * i, row = e / (DK / 8), c8 = e % (DK / 8);
+      const int at = 16 * (c8 / 2) + 4 * (c8 % 2);
+      uint2* kd = reinterpret_cast<uint2*>(kt + row * KS + at);
+      kd[0] = make_uint2(kr[i].x, kr[i].y);
+      kd[2] = make_uint2(kr[i].z, kr[i].w);
+      if constexpr (kOut) {
+        uint2* qd = reinterpret_cast<uint2*>(qt + row * QS + at);
+        qd[0] = make_uint2(qr[i].x, qr[i].y);
+        qd[2] = make_uint2(qr[i].z, qr[i].w);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VV; ++i) {
+      const int e = t + NT * i, row = e / (4 * NW), c8 = 8 * (e % (4 * NW));
+      *reinterpret_cast<uint4*>(vt + row * VS + c8) = vr[i];
+    }
+    if (wave == 0) {
+      double s = static_cast<double>(gr < kLeastLog ? kLeastLog : gr) * kLog2e;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const double y = __shfl_up(s, m, 64);
+        if (lane >= m) s += y;
+      }
+      const double all = __shfl(s, 63, 64);
+      run_log += all;
+      logs[lane] = s;
+      to_end[lane] = __builtin_amdgcn_exp2f(static_cast<float>(all - s));
+      from_start[lane] = __builtin_amdgcn_exp2f(static_cast<float>(s));
+    }
+    __syncthreads();
+    if (first + kChunk < count) load(first + kChunk);
+
+    f32x16 O[2];
+    if constexpr (kOut) {
+      // ---- scores of tiles (tokens j, tokens i): (0, 0), (0, 1), (1, 1)
+      for (int w = wave; w < 3; w += NW) {
+        const int jt = w >> 1, it = (w + 1) >> 1;
+        f32x16 A;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) A[r] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < DK / 16; ++s) {
+          const bf16x8 ka = *reinterpret_cast<const bf16x8*>(kt + (32 * jt + n32) * KS + 16 * s + 8 * half);
+          const bf16x8 qa = *reinterpret_cast<const bf16x8*>(qt + (32 * it + n32) * QS + 16 * s + 8 * half);
+          A = mfma(ka, qa, A);
+        }
+        const int i = 32 * it + n32;
+        const double li = logs[i];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float y[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const int j = 32 * jt + 16 * s + 8 * (r / 4) + 4 * half + r % 4;
+            const float d = __builtin_amdgcn_exp2f(static_cast<float>(li - logs[j]));
+            y[r] = j <= i ? A[8 * s + r] * d : 0.0f;
+          }
+          bf16x8 part[NP];
+          split8<NP>(y, part);
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            pt[((w * 2 + s) * NP + n) * 64 + lane] = __builtin_bit_cast(u32x4, part[n]);
+        }
+      }
+      // ---- S^T Q^T, then its decay from the chunk's start
+#pragma unroll
+      for (int it = 0; it < 2; ++it)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[it][r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < KT; ++c)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float y[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) y[r] = S[c][8 * s + r];
+          bf16x8 part[NP];
+          split8<NP>(y, part);
+#pragma unroll
+          for (int it = 0; it < 2; ++it) {
+            const bf16x8 qa = *reinterpret_cast<const bf16x8*>(qt + (32 * it + n32) * QS + 32 * c +
+                                                               16 * s + 8 * half);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) O[it] = mfma(part[n], qa, O[it]);
+          }
+        }
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+        const float d = from_start[32 * it + n32];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[it][r] *= d;
+      }
+      __syncthreads();  // P is there
+    }
+
+    // ---- V^T: lane n32 of a wave holds its column, 8 tokens of each 16
+    const int tr_row = 4 * half + (lane % 16) / 4, tr_col = 16 * ((lane / 16) & 1);
+    bf16x8 va[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      va[s] = read_columns8(vt + (16 * s + tr_row) * VS + 32 * wave + tr_col + 4 * (lane & 3),
+                            8 * VS);
+    if constexpr (kOut) {
+#pragma unroll
+      for (int it = 0; it < 2; ++it)
+#pragma unroll
+        for (int s = 0; s < 2 * (it + 1); ++s) {
+          const int w = (s >> 1) + it;  // tile (s / 2, it)
+#pragma unroll
+          for (int n = 0; n < NP; ++n)
+            O[it] = mfma(va[s], __builtin_bit_cast(bf16x8, pt[((w * 2 + (s & 1)) * NP + n) * 64 + lane]),
+                         O[it]);
+        }
+#pragma unroll
+      for (int it = 0; it < 2; ++it) {
+        const int i = first + 32 * it + n32;
+        if (i >= count) continue;
+        const size_t at = (static_cast<size_t>(tok0 + i) * p.HV + h) * p.dv;
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int c = col0 + 32 * wave + 8 * r4 + 4 * half;
+          if (c >= p.dv) continue;
+          const float o0 = p.scale * O[it][4 * r4], o1 = p.scale * O[it][4 * r4 + 1];
+          const float o2 = p.scale * O[it][4 * r4 + 2], o3 = p.scale * O[it][4 * r4 + 3];
+          if (p.o_bf16)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + at + c) =
+                make_uint2(pack_bf16x2(o0, o1), pack_bf16x2(o2, o3));
+          else
+            *reinterpret_cast<float4*>(static_cast<float*>(p.o) + at + c) =
+                make_float4(o0, o1, o2, o3);
+        }
+      }
+    }
+
+    // ---- S = exp(L_C) S + K^T (D V)
+    const float all = from_start[kChunk - 1];
+#pragma unroll
+    for (int c = 0; c < KT; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[c][r] *= all;
+    // the swapped quads: a lane's four channels 4 (lane & 3) of 16
+    const int k_quad = 4 * (((lane & 1) << 1) | ((lane >> 1) & 1));
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const float4 d0 = *reinterpret_cast<const float4*>(to_end + 16 * s + 4 * half);
+      const float4 d1 = *reinterpret_cast<const float4*>(to_end + 16 * s + 4 * half + 8);
+      const u32x4 w = __builtin_bit_cast(u32x4, va[s]);
+      float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
+                    bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
+                    bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
+      bf16x8 part[3];
+      split8<3>(y, part);
+#pragma unroll
+      for (int c = 0; c < KT; ++c) {
+        const bf16x8 ka = read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad,
+                                        8 * KS);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) S[c] = mfma(ka, part[n], S[c]);
+      }
     }
   }
-  if (padded || !keep || !in_row) return;
-  float* dst = reinterpret_cast<float*>(p.layer_base + to * p.slot_stride + h * p.tile_stride);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = rg + 32 * i;
-    if (r < p.dk)
-      *reinterpret_cast<float4*>(dst + static_cast<size_t>(r) * p.dv + col) =
-          make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+
+  // ---- the state after the last token
+  float* dst = nullptr;
+  if constexpr (kOut) {
+    if (seg == segs - 1 && keep)
+      dst = reinterpret_cast<float*>(p.layer_base + to * p.slot_stride + h * p.tile_stride);
+  } else {
+    dst = pp.seg_states + tile + seg * tile_step;
+    if (t == 0 && col0 == 0)
+      pp.seg_decays[(static_cast<size_t>(b) * pp.segments + seg) * p.HV + h] =
+          __builtin_amdgcn_exp2f(static_cast<float>(run_log));
   }
+  if (dst && col < p.dv) {
+#pragma unroll
+    for (int c = 0; c < KT; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
+        if (row < p.dk) dst[static_cast<size_t>(row) * p.dv + col] = S[c][r];
+      }
+  }
+}
+
+// The state before each segment of a request, in the place of what the
+// segment adds: X_0 = S_in, X_{s+1} = decay_s X_s + added_s.
+__global__ __launch_bounds__(256) void prompt_states(const PromptParams pp) {
+  const LinearParams& p = pp.l;
+  const int h = blockIdx.x, b = blockIdx.y;
+  int start, len;
+  request_range(pp, b, start, len);
+  const int segs = segments_of(pp, len);
+  const int from = p.slot_in[b];
+  const bool old = from >= 0 && from < p.num_slots;
+  const int at = (blockIdx.z * 256 + threadIdx.x) * 4;
+  if (segs < 2 || at >= p.dk * p.dv || (!old && from != DAMP_SLOT_ZERO)) return;
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (old)
+    x = *reinterpret_cast<const float4*>(p.layer_base + from * p.slot_stride + h * p.tile_stride +
+                                         static_cast<size_t>(at) * 4);
+  const size_t step = static_cast<size_t>(p.HV) * p.dk * p.dv;
+  float* state = pp.seg_states + static_cast<size_t>(b) * pp.segments * step +
+                 static_cast<size_t>(h) * p.dk * p.dv + at;
+  const float* decay = pp.seg_decays + static_cast<size_t>(b) * pp.segments * p.HV + h;
+  for (int s = 0; s < segs; ++s) {
+    float4* place = reinterpret_cast<float4*>(state + s * step);
+    const bool last = s == segs - 1;
+    const float4 add = last ? x : *place;
+    const float d = last ? 0.0f : decay[static_cast<size_t>(s) * p.HV];
+    *place = x;
+    x.x = fmaf(d, x.x, add.x);
+    x.y = fmaf(d, x.y, add.y);
+    x.z = fmaf(d, x.z, add.z);
+    x.w = fmaf(d, x.w, add.w);
+  }
+}
+
+// Tokens of a segment: requests are cut so that about kWorkgroups workgroups
+// have work, each at least kLeastSegment tokens. The lengths are on the
+// device, so the rule goes by B requests of max_len tokens.
+constexpr int kWorkgroups = 1024;
+constexpr int kLeastSegment = 256;
+
+struct Split {
+  int32_t seg_len, segments;
+};
+
+Split split_of(const damp_pool* pool, int32_t B, int32_t max_len) {
+  const int64_t heads = static_cast<int64_t>(pool->num_v_heads) * ((pool->layout.d_v + 127) / 128);
+  const int64_t chunks = (static_cast<int64_t>(max_len) + kChunk - 1) / kChunk;
+  int64_t seg = (chunks * B * heads + kWorkgroups - 1) / kWorkgroups * kChunk;
+  if (seg < kLeastSegment) seg = kLeastSegment;
+  seg = std::min<int64_t>(seg, 1 << 30);
+  return {static_cast<int32_t>(seg),
+          static_cast<int32_t>(std::max<int64_t>((max_len + seg - 1) / seg, 1))};
+}
+
+size_t workspace_bytes_of(const damp_pool* pool, int32_t B, const Split& s) {
+  if (s.segments < 2) return 0;
+  const size_t tiles = static_cast<size_t>(B) * s.segments * pool->num_v_heads;
+  return tiles * (static_cast<size_t>(pool->layout.d_k) * pool->layout.d_v + 1) * sizeof(float);
+}
+
+template <int DK, int NW>
+void launch(const PromptParams& p, int B, hipStream_t s) {
+  const int nx = p.l.HV * ((p.l.dv + 32 * NW - 1) / (32 * NW));
+  if (p.segments > 1) {
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 0>), dim3(nx, B, p.segments - 1), dim3(64 * NW), 0, s,
+                       p);
+    hipLaunchKernelGGL(prompt_states, dim3(p.l.HV, B, (p.l.dk * p.l.dv + 1023) / 1024), dim3(256),
+                       0, s, p);
+  }
+  if (p.l.o_bf16)
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 2>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+  else
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 3>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+}
+
+template <int DK>
+void launch_dk(const PromptParams& p, int B, hipStream_t s) {
+  if (p.l.dv <= 64) launch<DK, 2>(p, B, s);
+  else launch<DK, 4>(p, B, s);
 }
 
 }  // namespace
@@ -107,10 +499,9 @@ __global__ __launch_bounds__(256) void prompt_recurrent(const PromptParams pp) {
 extern "C" {
 
 size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B, int32_t max_len) {
-  (void)pool;
-  (void)B;
-  (void)max_len;
-  return 0;
+  using namespace damp;
+  if (check_pool(pool) != DAMP_OK || B <= 0 || B > 65535 || max_len < 0) return 0;
+  return workspace_bytes_of(pool, B, split_of(pool, B, max_len));
 }
 
 damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int32_t* slot_in,
@@ -138,7 +529,8 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
                                  q_stride, k, k_stride, v, v_stride, g, g_stride, scale, o,
                                  o_dtype, s, &p.l);
   if (st != DAMP_OK || B == 0) return st;
-  const size_t need = damp_linear_prefill_workspace_bytes(pool, B, max_len);
+  const Split split = split_of(pool, B, max_len);
+  const size_t need = workspace_bytes_of(pool, B, split);
   if (need > 0 && (!workspace || workspace_bytes < need ||
                    reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
     return fail(DAMP_ERR_INVALID_ARG, "%s: needs %zu bytes of 16-byte aligned workspace", name,
@@ -147,7 +539,13 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
   p.seq_len = seq_len;
   p.n_tokens = static_cast<int32_t>(n_tokens);
   p.max_len = max_len;
-  hipLaunchKernelGGL(prompt_recurrent, dim3(p.l.HV, B, (p.l.dv + 31) / 32), dim3(256), 0, s, p);
+  p.seg_len = split.seg_len;
+  p.segments = split.segments;
+  p.seg_states = static_cast<float*>(workspace);
+  p.seg_decays = p.seg_states + static_cast<size_t>(B) * split.segments * p.l.HV * p.l.dk * p.l.dv;
+  if (p.l.dk <= 64) launch_dk<64>(p, B, s);
+  else if (p.l.dk <= 128) launch_dk<128>(p, B, s);
+  else launch_dk<256>(p, B, s);
   return check_launch(name);
 }
 
