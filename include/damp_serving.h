@@ -92,7 +92,8 @@ size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B,
  *  workspace  damp_linear_prefill_workspace_bytes(pool, B, max_len) bytes,
  *             16-byte aligned (NULL where that is 0). Calls that may overlap
  *             need one each.
- * B = 0 is a no-op; B <= 65535; n_tokens < 2^31. */
+ * B = 0 is a no-op; B <= 65535; n_tokens < 2^31; token distances below 2^24
+ * and HV d_v below 2^23 elements. */
 damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer,
                                 const int32_t* slot_in, const int32_t* slot_out,
                                 int32_t B, int64_t n_tokens, int32_t max_len,

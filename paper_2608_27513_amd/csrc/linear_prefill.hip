@@ -42,9 +42,12 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
+constexpr int kBufferConfig = 0x00020000;  // raw 32-bit buffer (gfx9 family)
+constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer here
 constexpr float kLeastLog = -1000.0f;
 constexpr double kLog2e = 1.4426950408889634;
 
@@ -109,11 +112,47 @@ __device__ __forceinline__ bf16x8 read_columns8(const uint16_t* at, int step) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// The rows from `row0` on of a chunk as a buffer: reads of rows past `rows`
+// give zeros and writes to them are dropped. row_bytes * 64 < 2^31.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* base, int64_t row0,
+                                                          int64_t row_bytes, int rows) {
+  const int n = rows < kChunk ? rows : kChunk;
+  return __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(static_cast<const uint8_t*>(base)) + row0 * row_bytes, 0,
+      n * static_cast<int>(row_bytes), kBufferConfig);
+}
+
+// One head's state.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t state_buffer(const float* state,
+                                                               const LinearParams& p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(state), 0, p.dk * p.dv * 4,
+                                           kBufferConfig);
+}
+
+// Sum over the lanes up to this one (zeros come in from below).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_f64(double x) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(w), CTRL, ROWS, 0xf, false);
+  const uint32_t hi =
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(w >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_scan_f64(double x) {
+  x += dpp_f64<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+  x += dpp_f64<0x112, 0xf>(x);
+  x += dpp_f64<0x114, 0xf>(x);
+  x += dpp_f64<0x118, 0xf>(x);
+  x += dpp_f64<0x142, 0xa>(x);  // the last lane of each row of 16 into the next
+  x += dpp_f64<0x143, 0xc>(x);  // the last lane of the first half into the second
+  return x;
+}
+
 // PARTS = 0: the first pass, which leaves the state of each segment but the
 // last from a zero start. PARTS = 2 or 3: outputs, with so many parts of S
 // and P.
 template <int DK, int NW, int PARTS>
-__global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) {
+__global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(const PromptParams pp) {
   const LinearParams& p = pp.l;
   constexpr bool kOut = PARTS > 0;
   constexpr int NT = 64 * NW;
@@ -128,8 +167,10 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
   __shared__ __attribute__((aligned(16))) uint16_t qt[kOut ? kChunk * QS : 8];
   __shared__ __attribute__((aligned(16))) uint16_t vt[kChunk * VS];
   __shared__ u32x4 pt[kOut ? 3 * 2 * NP * 64 : 1];
-  __shared__ double logs[kChunk];
-  __shared__ float to_end[kChunk], from_start[kChunk];
+  __shared__ float2 logs[2][kChunk];  // L_i as a multiple of 2^-6 and the rest
+  __shared__ __attribute__((aligned(16))) float to_end[2][kChunk];
+  __shared__ float from_start[2][kChunk];  // times the scale
+  __shared__ float chunk_decay[2];
 
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int half = lane >> 5, n32 = lane & 31;
@@ -172,6 +213,10 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
   const int col = col0 + 32 * wave + n32;
   const size_t tile = (static_cast<size_t>(b) * pp.segments * p.HV + h) * p.dk * p.dv;
   const size_t tile_step = static_cast<size_t>(p.HV) * p.dk * p.dv;
+  // this lane's first row and column; rows and columns past the head are
+  // past the buffer's end
+  const uint32_t s_row = 4 * p.dv;
+  const uint32_t s_at = col < p.dv ? 4 * half * s_row + 4 * col : kNowhere;
   f32x16 S[KT];
 #pragma unroll
   for (int c = 0; c < KT; ++c)
@@ -183,83 +228,93 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
       src = pp.seg_states + tile + seg * tile_step;
     else if (old)
       src = reinterpret_cast<const float*>(p.layer_base + from * p.slot_stride + h * p.tile_stride);
-    if (src && col < p.dv) {
+    if (src) {
+      const auto sbuf = state_buffer(src, p);
 #pragma unroll
       for (int c = 0; c < KT; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
-          if (row < p.dk) S[c][r] = src[static_cast<size_t>(row) * p.dv + col];
-        }
+        for (int r = 0; r < 16; ++r)
+          S[c][r] = __uint_as_float(
+              __builtin_amdgcn_raw_buffer_load_b32(sbuf, s_at + s_row * (32 * c + 8 * (r / 4) + r % 4), 0, 0));
     }
   }
 
   // ---- loads of a chunk: rows past the end and columns past the head are zero
-  uint4 kr[KV], qr[kOut ? KV : 1], vr[VV];
-  float gr = 0.0f;
+  const int64_t k_row = 2 * p.k_stride, q_row = 2 * p.q_stride, v_row = 2 * p.v_stride;
+  const int64_t o_row = static_cast<int64_t>(p.HV) * p.dv * (p.o_bf16 ? 2 : 4);
+  constexpr int kRows = NT / (DK / 8), vRows = 16;  // rows that one load instruction spans
+  const int k8 = t % (DK / 8), v8 = t % (4 * NW);
+  const uint32_t k_at = 8 * k8 < p.dk ? t / (DK / 8) * static_cast<uint32_t>(k_row) + 16 * k8 : kNowhere;
+  const uint32_t q_at = 8 * k8 < p.dk ? t / (DK / 8) * static_cast<uint32_t>(q_row) + 16 * k8 : kNowhere;
+  const uint32_t v_at = col0 + 8 * v8 < p.dv ? t / (4 * NW) * static_cast<uint32_t>(v_row) + 16 * v8
+                                             : kNowhere;
+  u32x4 kr[KV], qr[kOut ? KV : 1], vr[VV];
   auto load = [&](int first) {
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const auto kbuf = rows_of(kb, tok0 + first, k_row, count - first);
+    const auto qbuf = rows_of(qb, tok0 + first, q_row, count - first);
+    const auto vbuf = rows_of(vb, tok0 + first, v_row, count - first);
 #pragma unroll
     for (int i = 0; i < KV; ++i) {
-      const int e = t + NT * i, row = e / (DK / 8), c8 = 8 * (e % (DK / 8));
-      const bool in = first + row < count && c8 < p.dk;
-      const int64_t tok = tok0 + first + row;
-      kr[i] = zero;
-      if (in) kr[i] = *reinterpret_cast<const uint4*>(kb + tok * p.k_stride + c8);
-      if constexpr (kOut) {
-        qr[i] = zero;
-        if (in) qr[i] = *reinterpret_cast<const uint4*>(qb + tok * p.q_stride + c8);
-      }
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          kbuf, k_at + i * kRows * static_cast<uint32_t>(k_row), 0, 0);
+      if constexpr (kOut)
+        qr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+            qbuf, q_at + i * kRows * static_cast<uint32_t>(q_row), 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < VV; ++i) {
-      const int e = t + NT * i, row = e / (4 * NW), c8 = 8 * (e % (4 * NW));
-      const bool in = first + row < count && col0 + c8 < p.dv;
-      vr[i] = zero;
-      if (in)
-        vr[i] = *reinterpret_cast<const uint4*>(vb + (tok0 + first + row) * p.v_stride + c8);
-    }
-    if (t < kChunk) gr = first + t < count ? gb[(tok0 + first + t) * p.g_stride] : 0.0f;
+    for (int i = 0; i < VV; ++i)
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          vbuf, v_at + i * vRows * static_cast<uint32_t>(v_row), 0, 0);
   };
 
-  double run_log = 0.0;  // of the segment so far, in the first wave
-  if (count > 0) load(0);
+  // ---- decays of a chunk, by the last wave, one chunk ahead of their use
+  const bool decays = wave == NW - 1;
+  float gr = 0.0f;
+  double run_log = 0.0;  // of the segment so far
+  auto load_g = [&](int first) {
+    gr = first + lane < count ? gb[(tok0 + first + lane) * p.g_stride] : 0.0f;
+  };
+  auto scan_g = [&](int to_buf) {
+    const double s = wave_scan_f64(static_cast<double>(gr < kLeastLog ? kLeastLog : gr) * kLog2e);
+    const double all = __shfl(s, 63, 64);
+    run_log += all;
+    const double coarse = __builtin_rint(s * 64.0) * 0.015625;
+    logs[to_buf][lane] = make_float2(static_cast<float>(coarse), static_cast<float>(s - coarse));
+    to_end[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(all - s));
+    from_start[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(s)) * p.scale;
+    if (lane == 0) chunk_decay[to_buf] = __builtin_amdgcn_exp2f(static_cast<float>(all));
+  };
+
+  if (count > 0) {
+    load(0);
+    if (decays) {
+      load_g(0);
+      scan_g(0);
+      load_g(kChunk);
+    }
+  }
   for (int first = 0; first < count; first += kChunk) {
+    const int buf = (first / kChunk) & 1;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < KV; ++i) {
       // quads 0 1 2 3 of 16 channels are stored as 0 2 1 3
-      const int e = t + NT * i, row = e / (DK / 8), c8 = e % (DK / 8);
-      const int at = 16 * (c8 / 2) + 4 * (c8 % 2);
+      const int row = t / (DK / 8) + kRows * i, at = 16 * (k8 / 2) + 4 * (k8 % 2);
       uint2* kd = reinterpret_cast<uint2*>(kt + row * KS + at);
-      kd[0] = make_uint2(kr[i].x, kr[i].y);
-      kd[2] = make_uint2(kr[i].z, kr[i].w);
+      kd[0] = make_uint2(kr[i][0], kr[i][1]);
+      kd[2] = make_uint2(kr[i][2], kr[i][3]);
       if constexpr (kOut) {
         uint2* qd = reinterpret_cast<uint2*>(qt + row * QS + at);
-        qd[0] = make_uint2(qr[i].x, qr[i].y);
-        qd[2] = make_uint2(qr[i].z, qr[i].w);
+        qd[0] = make_uint2(qr[i][0], qr[i][1]);
+        qd[2] = make_uint2(qr[i][2], qr[i][3]);
       }
     }
 #pragma unroll
-    for (int i = 0; i < VV; ++i) {
-      const int e = t + NT * i, row = e / (4 * NW), c8 = 8 * (e % (4 * NW));
-      *reinterpret_cast<uint4*>(vt + row * VS + c8) = vr[i];
-    }
-    if (wave == 0) {
-      double s = static_cast<double>(gr < kLeastLog ? kLeastLog : gr) * kLog2e;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const double y = __shfl_up(s, m, 64);
-        if (lane >= m) s += y;
-      }
-      const double all = __shfl(s, 63, 64);
-      run_log += all;
-      logs[lane] = s;
-      to_end[lane] = __builtin_amdgcn_exp2f(static_cast<float>(all - s));
-      from_start[lane] = __builtin_amdgcn_exp2f(static_cast<float>(s));
-    }
+    for (int i = 0; i < VV; ++i)
+      *reinterpret_cast<u32x4*>(vt + (t / (4 * NW) + vRows * i) * VS + 8 * v8) = vr[i];
     __syncthreads();
-    if (first + kChunk < count) load(first + kChunk);
+    const bool more = first + kChunk < count;
+    if (more) load(first + kChunk);
 
     f32x16 O[2];
     if constexpr (kOut) {
@@ -276,15 +331,18 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
           A = mfma(ka, qa, A);
         }
         const int i = 32 * it + n32;
-        const double li = logs[i];
+        const float2 li = logs[buf][i];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           float y[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const int j = 32 * jt + 16 * s + 8 * (r / 4) + 4 * half + r % 4;
-            const float d = __builtin_amdgcn_exp2f(static_cast<float>(li - logs[j]));
-            y[r] = j <= i ? A[8 * s + r] * d : 0.0f;
+            const float2 lj = logs[buf][j];
+            float a = A[8 * s + r] * p.scale;
+            a *= __builtin_amdgcn_exp2f((li.x - lj.x) + (li.y - lj.y));
+            asm("" : "+v"(a));  // all of it before the mask: no branch for each value
+            y[r] = j <= i ? a : 0.0f;
           }
           bf16x8 part[NP];
           split8<NP>(y, part);
@@ -292,6 +350,10 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
           for (int n = 0; n < NP; ++n)
             pt[((w * 2 + s) * NP + n) * 64 + lane] = __builtin_bit_cast(u32x4, part[n]);
         }
+      }
+      if (decays && more) {
+        scan_g(buf ^ 1);
+        load_g(first + 2 * kChunk);
       }
       // ---- S^T Q^T, then its decay from the chunk's start
 #pragma unroll
@@ -317,7 +379,7 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
         }
 #pragma unroll
       for (int it = 0; it < 2; ++it) {
-        const float d = from_start[32 * it + n32];
+        const float d = from_start[buf][32 * it + n32];
 #pragma unroll
         for (int r = 0; r < 16; ++r) O[it][r] *= d;
       }
@@ -342,29 +404,38 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
             O[it] = mfma(va[s], __builtin_bit_cast(bf16x8, pt[((w * 2 + (s & 1)) * NP + n) * 64 + lane]),
                          O[it]);
         }
+      const auto obuf = rows_of(static_cast<uint8_t*>(p.o) + (static_cast<int64_t>(h) * p.dv + col0) *
+                                                                 (p.o_bf16 ? 2 : 4),
+                                tok0 + first, o_row, count - first);
 #pragma unroll
       for (int it = 0; it < 2; ++it) {
-        const int i = first + 32 * it + n32;
-        if (i >= count) continue;
-        const size_t at = (static_cast<size_t>(tok0 + i) * p.HV + h) * p.dv;
+        const uint32_t row_at = (32 * it + n32) * static_cast<uint32_t>(o_row);
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-          const int c = col0 + 32 * wave + 8 * r4 + 4 * half;
-          if (c >= p.dv) continue;
-          const float o0 = p.scale * O[it][4 * r4], o1 = p.scale * O[it][4 * r4 + 1];
-          const float o2 = p.scale * O[it][4 * r4 + 2], o3 = p.scale * O[it][4 * r4 + 3];
-          if (p.o_bf16)
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.o) + at + c) =
-                make_uint2(pack_bf16x2(o0, o1), pack_bf16x2(o2, o3));
-          else
-            *reinterpret_cast<float4*>(static_cast<float*>(p.o) + at + c) =
-                make_float4(o0, o1, o2, o3);
+          const int c = 32 * wave + 8 * r4 + 4 * half;
+          const bool in = col0 + c < p.dv;
+          const f32x16& y = O[it];
+          if (p.o_bf16) {
+            const u32x2 w = {pack_bf16x2(y[4 * r4], y[4 * r4 + 1]),
+                             pack_bf16x2(y[4 * r4 + 2], y[4 * r4 + 3])};
+            __builtin_amdgcn_raw_buffer_store_b64(w, obuf, in ? row_at + 2 * c : kNowhere, 0, 0);
+          } else {
+            const u32x4 w = {__float_as_uint(y[4 * r4]), __float_as_uint(y[4 * r4 + 1]),
+                             __float_as_uint(y[4 * r4 + 2]), __float_as_uint(y[4 * r4 + 3])};
+            __builtin_amdgcn_raw_buffer_store_b128(w, obuf, in ? row_at + 4 * c : kNowhere, 0, 0);
+          }
         }
       }
+    } else if (decays && more) {
+      scan_g(buf ^ 1);
+      load_g(first + 2 * kChunk);
     }
 
     // ---- S = exp(L_C) S + K^T (D V)
-    const float all = from_start[kChunk - 1];
+    // the third part is for a state that is kept; one that only o in bf16 is
+    // read from has enough of two
+    const bool whole = PARTS != 2 || (seg == segs - 1 && keep);
+    const float all = chunk_decay[buf];
 #pragma unroll
     for (int c = 0; c < KT; ++c)
 #pragma unroll
@@ -373,21 +444,24 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
     const int k_quad = 4 * (((lane & 1) << 1) | ((lane >> 1) & 1));
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const float4 d0 = *reinterpret_cast<const float4*>(to_end + 16 * s + 4 * half);
-      const float4 d1 = *reinterpret_cast<const float4*>(to_end + 16 * s + 4 * half + 8);
+      const float4 d0 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half);
+      const float4 d1 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half + 8);
       const u32x4 w = __builtin_bit_cast(u32x4, va[s]);
       float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
                     bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
                     bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
       bf16x8 part[3];
       split8<3>(y, part);
+      bf16x8 ka[KT];
 #pragma unroll
       for (int c = 0; c < KT; ++c) {
-        const bf16x8 ka = read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad,
-                                        8 * KS);
+        ka[c] = read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
 #pragma unroll
-        for (int n = 0; n < 3; ++n) S[c] = mfma(ka, part[n], S[c]);
+        for (int n = 0; n < 2; ++n) S[c] = mfma(ka[c], part[n], S[c]);
       }
+      if (whole)
+#pragma unroll
+        for (int c = 0; c < KT; ++c) S[c] = mfma(ka[c], part[2], S[c]);
     }
   }
 
@@ -398,18 +472,18 @@ __global__ __launch_bounds__(64 * NW) void prompt_chunks(const PromptParams pp) 
       dst = reinterpret_cast<float*>(p.layer_base + to * p.slot_stride + h * p.tile_stride);
   } else {
     dst = pp.seg_states + tile + seg * tile_step;
-    if (t == 0 && col0 == 0)
+    if (decays && lane == 0 && col0 == 0)
       pp.seg_decays[(static_cast<size_t>(b) * pp.segments + seg) * p.HV + h] =
           __builtin_amdgcn_exp2f(static_cast<float>(run_log));
   }
-  if (dst && col < p.dv) {
+  if (dst) {
+    const auto sbuf = state_buffer(dst, p);
 #pragma unroll
     for (int c = 0; c < KT; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = 32 * c + 8 * (r / 4) + 4 * half + r % 4;
-        if (row < p.dk) dst[static_cast<size_t>(row) * p.dv + col] = S[c][r];
-      }
+      for (int r = 0; r < 16; ++r)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[c][r]), sbuf,
+                                              s_at + s_row * (32 * c + 8 * (r / 4) + r % 4), 0, 0);
   }
 }
 
@@ -529,6 +603,11 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
                                  q_stride, k, k_stride, v, v_stride, g, g_stride, scale, o,
                                  o_dtype, s, &p.l);
   if (st != DAMP_OK || B == 0) return st;
+  // a chunk's rows are addressed with 31 bits
+  constexpr int64_t kMost = (int64_t{1} << 31) / kChunk / 4 - 8;
+  if (q_stride > 2 * kMost || k_stride > 2 * kMost || v_stride > 2 * kMost ||
+      static_cast<int64_t>(p.l.HV) * p.l.dv > kMost)
+    return fail(DAMP_ERR_INVALID_ARG, "%s: a token's row is too long", name);
   const Split split = split_of(pool, B, max_len);
   const size_t need = workspace_bytes_of(pool, B, split);
   if (need > 0 && (!workspace || workspace_bytes < need ||
