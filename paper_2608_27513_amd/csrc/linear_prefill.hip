@@ -14,9 +14,10 @@
 // lane in the order that the next product wants its operand: with
 //   k slots (lane half h, j = 0 .. 7)  <->  rows 16 s + 4 h + j (+ 4 if j > 3)
 // the state's accumulators are S^T's operand and the scores' are P^T's without
-// leaving the lane. Q and K are stored in LDS with the middle two quads of
-// every 16 channels swapped, so that these 8 rows are 16 neighbouring bytes;
-// K^T and V^T come through transposing LDS reads.
+// leaving the lane. The state's rows are key channels in an order that makes
+// these 8 rows 8 neighbouring channels (the middle two quads of every 16 are
+// swapped), so that K and Q are read as they are; K^T and V^T come through
+// transposing LDS reads.
 //
 // q, k, v are bf16 and enter as they are. What is fp32 (S, P, D V) enters as
 // a sum of bf16 parts, x = x1 + x2 (+ x3), each the rounding of what the
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   // this lane's first row and column; rows and columns past the head are
   // past the buffer's end
   const uint32_t s_row = 4 * p.dv;
-  const uint32_t s_at = col < p.dv ? 4 * half * s_row + 4 * col : kNowhere;
+  const uint32_t s_at = col < p.dv ? 8 * half * s_row + 4 * col : kNowhere;
   f32x16 S[KT];
 #pragma unroll
   for (int c = 0; c < KT; ++c)
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           S[c][r] = __uint_as_float(
-              __builtin_amdgcn_raw_buffer_load_b32(sbuf, s_at + s_row * (32 * c + 8 * (r / 4) + r % 4), 0, 0));
+              __builtin_amdgcn_raw_buffer_load_b32(sbuf, s_at + s_row * (32 * c + 16 * (r / 8) + r % 8), 0, 0));
     }
   }
 
@@ -285,6 +286,18 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     if (lane == 0) chunk_decay[to_buf] = __builtin_amdgcn_exp2f(static_cast<float>(all));
   };
 
+  auto stage = [&] {
+#pragma unroll
+    for (int i = 0; i < KV; ++i) {
+      const int row = t / (DK / 8) + kRows * i;
+      *reinterpret_cast<u32x4*>(kt + row * KS + 8 * k8) = kr[i];
+      if constexpr (kOut) *reinterpret_cast<u32x4*>(qt + row * QS + 8 * k8) = qr[i];
+    }
+#pragma unroll
+    for (int i = 0; i < VV; ++i)
+      *reinterpret_cast<u32x4*>(vt + (t / (4 * NW) + vRows * i) * VS + 8 * v8) = vr[i];
+  };
+
   if (count > 0) {
     load(0);
     if (decays) {
@@ -292,29 +305,13 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       scan_g(0);
       load_g(kChunk);
     }
+    stage();
+    if (kChunk < count) load(kChunk);
   }
   for (int first = 0; first < count; first += kChunk) {
     const int buf = (first / kChunk) & 1;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < KV; ++i) {
-      // quads 0 1 2 3 of 16 channels are stored as 0 2 1 3
-      const int row = t / (DK / 8) + kRows * i, at = 16 * (k8 / 2) + 4 * (k8 % 2);
-      uint2* kd = reinterpret_cast<uint2*>(kt + row * KS + at);
-      kd[0] = make_uint2(kr[i][0], kr[i][1]);
-      kd[2] = make_uint2(kr[i][2], kr[i][3]);
-      if constexpr (kOut) {
-        uint2* qd = reinterpret_cast<uint2*>(qt + row * QS + at);
-        qd[0] = make_uint2(qr[i][0], qr[i][1]);
-        qd[2] = make_uint2(qr[i][2], qr[i][3]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < VV; ++i)
-      *reinterpret_cast<u32x4*>(vt + (t / (4 * NW) + vRows * i) * VS + 8 * v8) = vr[i];
-    __syncthreads();
     const bool more = first + kChunk < count;
-    if (more) load(first + kChunk);
+    __syncthreads();  // the chunk is there
 
     f32x16 O[2];
     if constexpr (kOut) {
@@ -351,10 +348,6 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
             pt[((w * 2 + s) * NP + n) * 64 + lane] = __builtin_bit_cast(u32x4, part[n]);
         }
       }
-      if (decays && more) {
-        scan_g(buf ^ 1);
-        load_g(first + 2 * kChunk);
-      }
       // ---- S^T Q^T, then its decay from the chunk's start
 #pragma unroll
       for (int it = 0; it < 2; ++it)
@@ -383,7 +376,6 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
 #pragma unroll
         for (int r = 0; r < 16; ++r) O[it][r] *= d;
       }
-      __syncthreads();  // P is there
     }
 
     // ---- V^T: lane n32 of a wave holds its column, 8 tokens of each 16
@@ -393,6 +385,48 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     for (int s = 0; s < 4; ++s)
       va[s] = read_columns8(vt + (16 * s + tr_row) * VS + 32 * wave + tr_col + 4 * (lane & 3),
                             8 * VS);
+    // ---- S = exp(L_C) S + K^T (D V)
+    // the third part is for a state that is kept; one that only o in bf16 is
+    // read from has enough of two
+    const bool whole = PARTS != 2 || (seg == segs - 1 && keep);
+    const float all = chunk_decay[buf];
+#pragma unroll
+    for (int c = 0; c < KT; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[c][r] *= all;
+    // the state's row order: the quads of 16 channels as 0 2 1 3
+    const int k_quad = 4 * (((lane & 1) << 1) | ((lane >> 1) & 1));
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const float4 d0 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half);
+      const float4 d1 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half + 8);
+      const u32x4 w = __builtin_bit_cast(u32x4, va[s]);
+      float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
+                    bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
+                    bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
+      bf16x8 part[3];
+      split8<3>(y, part);
+      bf16x8 ka[KT];
+#pragma unroll
+      for (int c = 0; c < KT; ++c) {
+        ka[c] = read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) S[c] = mfma(ka[c], part[n], S[c]);
+      }
+      if (whole)
+#pragma unroll
+        for (int c = 0; c < KT; ++c) S[c] = mfma(ka[c], part[2], S[c]);
+    }
+  
+    // ---- the next decays; then P is there, and K, Q and V have been read
+    if (decays && more) {
+      scan_g(buf ^ 1);
+      load_g(first + 2 * kChunk);
+    }
+    __syncthreads();
+    if (more) stage();
+    if (first + 2 * kChunk < count) load(first + 2 * kChunk);
+    // ---- O += V^T P^T
     if constexpr (kOut) {
 #pragma unroll
       for (int it = 0; it < 2; ++it)
@@ -426,42 +460,6 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
           }
         }
       }
-    } else if (decays && more) {
-      scan_g(buf ^ 1);
-      load_g(first + 2 * kChunk);
-    }
-
-    // ---- S = exp(L_C) S + K^T (D V)
-    // the third part is for a state that is kept; one that only o in bf16 is
-    // read from has enough of two
-    const bool whole = PARTS != 2 || (seg == segs - 1 && keep);
-    const float all = chunk_decay[buf];
-#pragma unroll
-    for (int c = 0; c < KT; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) S[c][r] *= all;
-    // the swapped quads: a lane's four channels 4 (lane & 3) of 16
-    const int k_quad = 4 * (((lane & 1) << 1) | ((lane >> 1) & 1));
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const float4 d0 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half);
-      const float4 d1 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half + 8);
-      const u32x4 w = __builtin_bit_cast(u32x4, va[s]);
-      float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
-                    bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
-                    bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
-      bf16x8 part[3];
-      split8<3>(y, part);
-      bf16x8 ka[KT];
-#pragma unroll
-      for (int c = 0; c < KT; ++c) {
-        ka[c] = read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) S[c] = mfma(ka[c], part[n], S[c]);
-      }
-      if (whole)
-#pragma unroll
-        for (int c = 0; c < KT; ++c) S[c] = mfma(ka[c], part[2], S[c]);
     }
   }
 
@@ -483,7 +481,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[c][r]), sbuf,
-                                              s_at + s_row * (32 * c + 8 * (r / 4) + r % 4), 0, 0);
+                                              s_at + s_row * (32 * c + 16 * (r / 8) + r % 8), 0, 0);
   }
 }
 
