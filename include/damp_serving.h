@@ -140,9 +140,11 @@ size_t damp_verify_workspace_bytes(int32_t B, int32_t V);
  *  u          fp32 [B, K + 1]; u[b, K] draws the next token.
  *  accepted   int32 [B]: a.
  *  out        int32 [B, K + 1]: the drafts that stand, the next token, then -1.
- *  workspace  damp_verify_workspace_bytes(B, V) bytes, 16-byte aligned, all
- *             zero before its first call; every call leaves it zero again.
- *             Calls that may overlap need one each.
+ *  workspace  damp_verify_workspace_bytes(B, V) bytes (or more), 16-byte
+ *             aligned, its first 2^18 bytes zero before its first call; every
+ *             call leaves those zero again, so that a workspace serves call
+ *             after call, of any sizes that it has room for. Calls that may
+ *             overlap need one each.
  * K = 0 draws one token from p (q and tokens are not used). B = 0 is a no-op;
  * B <= 65535, 0 <= K <= 1024, 1 <= V <= 2^22. */
 damp_status damp_verify_drafts(const void* p, const void* q, int32_t dtype,

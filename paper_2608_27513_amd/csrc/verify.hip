@@ -2,11 +2,16 @@
 // the next token drawn from what the target has over the draft.
 //
 // One row of V weights is summed and searched for each request (its first
-// refused draft's, or the one after its last), so the row's bytes bound the
-// operator. A row is cut into tiles, one workgroup each; weights are whole
-// numbers of 2^-40, so the tiles' sums are exact in any order. A second kernel
-// finds the tile in which the running sum passes the drawn threshold and
-// scans that tile again.
+// refused draft's, or the one after its last), so the row's bytes, of p and
+// after a refusal of q, bound the operator; short rows are bound by the chain
+// lens -> tokens -> their probabilities -> the row.
+//
+// Weights are whole numbers of 2^-40, so sums are exact in any order. A wave
+// takes 64 vectors of 16 bytes of the row (a "piece") at a time and leaves the
+// piece's sum; the last workgroup of a request to finish (a ticket, so nothing
+// waits) runs over the sums to the piece that the drawn threshold falls into
+// and scans that one again. The largest rows are read once by many workgroups
+// and the rest of the work is a few kilobytes, in one launch.
 #include "device.hpp"
 #include "internal.hpp"
 
@@ -14,8 +19,9 @@ namespace damp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 4096;  // tokens of a tile
+constexpr int kWaves = kThreads / 64;
 constexpr int kMaxDrafts = 1024;
+constexpr int kAhead = 4;  // pieces of a wave in flight
 
 struct VerifyParams {
   const void* p;
@@ -25,142 +31,280 @@ struct VerifyParams {
   const float* u;
   int32_t* accepted;
   int32_t* out;
-  uint64_t* sums;  // [B, tiles]
-  int32_t K, V, tiles;
+  uint32_t* tickets;  // [65536], zero between calls
+  uint64_t* sums;     // [B, pieces]
+  int32_t K, V;
+  int32_t pieces;  // of a row
+  int32_t steps;   // pieces of a wave
 };
 
 template <typename T>
-__device__ __forceinline__ float prob(const T* row, int x) {
-  if constexpr (sizeof(T) == 4) return row[x];
-  else return bf16_to_f32(row[x]);
+constexpr int vec() {
+  return 16 / static_cast<int>(sizeof(T));
 }
 
-// floor(2^40 min(max(y, 0), 1)), in two exact steps of 20 bits each.
-__device__ __forceinline__ uint64_t fix40(float y) {
-  y = y > 0.0f ? fminf(y, 1.0f) : 0.0f;
-  const float up = y * 1048576.0f;
-  const uint32_t hi = static_cast<uint32_t>(up);
-  const uint32_t lo = static_cast<uint32_t>((up - static_cast<float>(hi)) * 1048576.0f);
-  return (static_cast<uint64_t>(hi) << 20) + lo;
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(uint16_t x) { return bf16_to_f32(x); }
+
+// vec<T>() values from x on, zero from V on. Rows start anywhere (V is any
+// number), which wide loads may do here.
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Vec {
+  T v[vec<T>()];
+};
+template <typename T>
+__device__ __forceinline__ Vec<T> load_vec(const T* row, int x, int V) {
+  Vec<T> r;
+  if (x + vec<T>() <= V) {
+    r = *reinterpret_cast<const Vec<T>*>(row + x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < vec<T>(); ++i) {
+      r.v[i] = 0;
+      if (x + i < V) r.v[i] = row[x + i];
+    }
+  }
+  return r;
+}
+
+// floor(2^40 min(max(y, 0), 1)) (0 for NaN) as hi 2^20 + lo, in exact steps of
+// 20 bits.
+__device__ __forceinline__ void fix40(float y, int& hi, int& lo) {
+  const float up = __builtin_amdgcn_fmed3f(y, 0.0f, 1.0f) * 1048576.0f;
+  const float whole = floorf(up);
+  hi = static_cast<int>(whole);
+  lo = static_cast<int>((up - whole) * 1048576.0f);
+}
+
+// The weight of a token as hi 2^20 + lo (lo may be negative).
+__device__ __forceinline__ void weight(float p, float q, int& hi, int& lo) {
+  int hp, lp, hq, lq;
+  fix40(p, hp, lp);
+  fix40(q, hq, lq);
+  const bool over = hp > hq || (hp == hq && lp > lq);
+  hi = over ? hp - hq : 0;
+  lo = over ? lp - lq : 0;
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_i32(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+// Sum over a wave, in lane 63.
+__device__ __forceinline__ int wave_sum_i32(int x) {
+  x += dpp_i32<0x111, 0xf>(x);
+  x += dpp_i32<0x112, 0xf>(x);
+  x += dpp_i32<0x114, 0xf>(x);
+  x += dpp_i32<0x118, 0xf>(x);
+  x += dpp_i32<0x142, 0xa>(x);
+  x += dpp_i32<0x143, 0xc>(x);
+  return x;
+}
+// Sum over the lanes before this one.
+__device__ __forceinline__ uint64_t wave_before_u64(uint64_t x) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long s = x;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const unsigned long long y = __shfl_up(s, m, 64);
+    if (lane >= m) s += y;
+  }
+  return s - x;
+}
+
+template <typename T, bool REFUSED>
+__device__ __forceinline__ uint64_t vec_weight(const Vec<T>& p, const Vec<T>& q, int i) {
+  int hi, lo;
+  if constexpr (REFUSED) weight(widen(p.v[i]), widen(q.v[i]), hi, lo);
+  else fix40(widen(p.v[i]), hi, lo);
+  return (static_cast<uint64_t>(hi) << 20) + static_cast<uint64_t>(static_cast<int64_t>(lo));
+}
+
+// The sums of this wave's pieces.
+template <typename T, bool REFUSED>
+__device__ __forceinline__ void sum_pieces(const VerifyParams& v, const T* p, const T* q,
+                                           uint64_t* sums, int piece0) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < v.steps; s0 += kAhead) {
+    Vec<T> pv[kAhead], qv[kAhead];
+    const int piece = piece0 + s0;
+    if (s0 + kAhead <= v.steps && (piece + kAhead) * 64 * vec<T>() <= v.V) {
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        const int x = ((piece + s) * 64 + lane) * vec<T>();
+        pv[s] = *reinterpret_cast<const Vec<T>*>(p + x);
+        if constexpr (REFUSED) qv[s] = *reinterpret_cast<const Vec<T>*>(q + x);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        const int x = ((piece + s) * 64 + lane) * vec<T>();
+        const int end = s0 + s < v.steps ? v.V : 0;
+        pv[s] = load_vec(p, x, end);
+        if constexpr (REFUSED) qv[s] = load_vec(q, x, end);
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      if (s0 + s >= v.steps || piece + s >= v.pieces) break;
+      int hi = 0, lo = 0;
+#pragma unroll
+      for (int i = 0; i < vec<T>(); ++i) {
+        int h, l;
+        if constexpr (REFUSED) weight(widen(pv[s].v[i]), widen(qv[s].v[i]), h, l);
+        else fix40(widen(pv[s].v[i]), h, l);
+        hi += h;  // at most 2^9 weights of 2^20
+        lo += l;
+      }
+      hi = wave_sum_i32(hi);
+      lo = wave_sum_i32(lo);
+      if (lane == 63)
+        __hip_atomic_store(&sums[piece + s],
+                           (static_cast<uint64_t>(hi) << 20) + static_cast<int64_t>(lo),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+}
+
+// The token in which the running sum passes `left`, in the piece that it does.
+template <typename T, bool REFUSED>
+__device__ __forceinline__ void draw_in_piece(const VerifyParams& v, const T* p, const T* q,
+                                              int piece, uint64_t left, int* next) {
+  const int x = (piece * 64 + (threadIdx.x & 63)) * vec<T>();
+  const Vec<T> pv = load_vec(p, x, v.V);
+  Vec<T> qv = pv;
+  if constexpr (REFUSED) qv = load_vec(q, x, v.V);
+  uint64_t s = 0;
+#pragma unroll
+  for (int i = 0; i < vec<T>(); ++i) s += vec_weight<T, REFUSED>(pv, qv, i);
+  uint64_t before = wave_before_u64(s);
+  if (left < before || left >= before + s) return;
+  int at = 0;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < vec<T>(); ++i) {
+    before += vec_weight<T, REFUSED>(pv, qv, i);
+    if (!found && left < before) {
+      found = true;
+      at = x + i;
+    }
+  }
+  *next = at;
 }
 
 template <typename T>
-__device__ __forceinline__ uint64_t weight(const T* p, const T* q, int x) {
-  const uint64_t a = fix40(prob(p, x));
-  if (!q) return a;
-  const uint64_t b = fix40(prob(q, x));
-  return a > b ? a - b : 0;
-}
+__global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) {
+  __shared__ int first, last, found_piece, next;
+  __shared__ uint64_t found_left, wave_total[kWaves];
+  const int b = blockIdx.y, t = threadIdx.x, lane = t & 63, wave = t >> 6;
 
-// The drafts of request b that stand; every thread receives the number.
-template <typename T>
-__device__ int drafts_that_stand(const VerifyParams& v, int b, int& n) {
-  __shared__ int first;
-  n = v.lens ? min(max(v.lens[b], 0), v.K) : v.K;
-  if (threadIdx.x == 0) first = n;
+  // ---- the drafts that stand
+  const int n = v.lens ? min(max(v.lens[b], 0), v.K) : v.K;
+  if (t == 0) {
+    first = n;
+    next = -1;
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  for (int i = t; i < n; i += kThreads) {
     const int x = v.tokens[static_cast<size_t>(b) * v.K + i];
     bool stands = x >= 0 && x < v.V;
     if (stands) {
       const size_t row = static_cast<size_t>(b) * v.K + i;
-      const T* p = static_cast<const T*>(v.p) + (row + b) * v.V;
-      const T* q = static_cast<const T*>(v.q) + row * v.V;
+      const float px = widen(static_cast<const T*>(v.p)[(row + b) * v.V + x]);
+      const float qx = widen(static_cast<const T*>(v.q)[row * v.V + x]);
       // the product of two fp32 numbers is exact in double
-      stands = static_cast<double>(v.u[row + b]) * static_cast<double>(prob(q, x)) <
-               static_cast<double>(prob(p, x));
+      stands = static_cast<double>(v.u[row + b]) * static_cast<double>(qx) < static_cast<double>(px);
     }
     if (!stands) atomicMin(&first, i);
   }
   __syncthreads();
-  return first;
-}
-
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(static_cast<unsigned long long>(x), m, 64);
-  return x;
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_sums(const VerifyParams v) {
-  __shared__ uint64_t part[kThreads / 64];
-  const int b = blockIdx.y, t = threadIdx.x;
-  int n;
-  const int a = drafts_that_stand<T>(v, b, n);
+  const int a = first;
+  const bool refused = a < n;
   const T* p = static_cast<const T*>(v.p) + (static_cast<size_t>(b) * (v.K + 1) + a) * v.V;
-  const T* q = a < n ? static_cast<const T*>(v.q) + (static_cast<size_t>(b) * v.K + a) * v.V
-                     : nullptr;
-  const int x0 = blockIdx.x * kTile, x1 = min(x0 + kTile, v.V);
-  uint64_t s = 0;
-  for (int x = x0 + t; x < x1; x += kThreads) s += weight(p, q, x);
-  s = wave_sum_u64(s);
-  if ((t & 63) == 0) part[t >> 6] = s;
+  const T* q = static_cast<const T*>(v.q) + (static_cast<size_t>(b) * v.K + a) * v.V;
+
+  // ---- the sums of this workgroup's pieces
+  uint64_t* sums = v.sums + static_cast<size_t>(b) * v.pieces;
+  const int piece0 = (static_cast<int>(blockIdx.x) * kWaves + wave) * v.steps;
+  if (refused) sum_pieces<T, true>(v, p, q, sums, piece0);
+  else sum_pieces<T, false>(v, p, q, sums, piece0);
+  // The sums go through agent-scope atomic stores and loads, which pass the
+  // L2 of their XCD, so they are in order with the ticket as soon as the stores
+  // are acknowledged. A release fence would do, but writes back the whole L2
+  // for each workgroup (270 us against 28 at 128 requests of 151001 tokens).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (t == 0)
-    v.sums[static_cast<size_t>(b) * v.tiles + blockIdx.x] =
-        (part[0] + part[1]) + (part[2] + part[3]);
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_draw(const VerifyParams v) {
-  __shared__ uint64_t before[kThreads];
-  __shared__ uint64_t rest;
-  __shared__ int found;
-  const int b = blockIdx.x, t = threadIdx.x;
-  int n;
-  const int a = drafts_that_stand<T>(v, b, n);
-  const T* p = static_cast<const T*>(v.p) + (static_cast<size_t>(b) * (v.K + 1) + a) * v.V;
-  const T* q = a < n ? static_cast<const T*>(v.q) + (static_cast<size_t>(b) * v.K + a) * v.V
-                     : nullptr;
   if (t == 0) {
-    const uint64_t* sums = v.sums + static_cast<size_t>(b) * v.tiles;
-    uint64_t total = 0;
-    for (int i = 0; i < v.tiles; ++i) total += sums[i];
-    const float u = v.u[static_cast<size_t>(b) * (v.K + 1) + v.K];
-    const uint32_t r = u > 0.0f ? min(static_cast<uint32_t>(fminf(u, 1.0f) * 16777216.0f), 0xffffffu)
-                                : 0u;
-    uint64_t left = (total >> 24) * r + (((total & 0xffffffu) * r) >> 24);
-    int tile = -1;
-    if (total > 0)
-      for (tile = 0; left >= sums[tile]; ++tile) left -= sums[tile];
-    rest = left;
-    found = tile;
+    const uint32_t ticket =
+        __hip_atomic_fetch_add(&v.tickets[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = ticket == gridDim.x - 1;
+    if (last) __hip_atomic_store(&v.tickets[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  const int tile = found;
-  int next = -1;
-  if (tile >= 0) {
-    // thread t sums its run of the tile's tokens; the run that the threshold
-    // falls into is walked by its thread
-    const int run = kTile / kThreads;
-    const int x0 = tile * kTile + t * run, x1 = min(x0 + run, v.V);
-    uint64_t s = 0;
-    for (int x = x0; x < x1; ++x) s += weight(p, q, x);
-    before[t] = s;
-    __syncthreads();
-    uint64_t sum = 0;
-    for (int i = 0; i < t; ++i) sum += before[i];
-    if (rest >= sum && rest < sum + s) {
-      uint64_t left = rest - sum;
-      for (int x = x0; x < x1; ++x) {
-        const uint64_t w = weight(p, q, x);
-        if (left < w) {
-          next = x;
-          break;
-        }
-        left -= w;
-      }
-      found = next;
-    }
-    __syncthreads();
-    next = found;
+  if (!last) return;
+
+  // ---- the last of a request: the piece that the threshold falls into
+  const int each = (v.pieces + kThreads - 1) / kThreads;
+  const int i0 = min(t * each, v.pieces), i1 = min(i0 + each, v.pieces);
+  auto sum_of = [&](int i) {
+    return __hip_atomic_load(&sums[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  uint64_t s = 0;
+  for (int i = i0; i < i1; ++i) s += sum_of(i);
+  uint64_t before = wave_before_u64(s);
+  if (lane == 63) wave_total[wave] = before + s;
+  if (t == 0) found_piece = -1;
+  __syncthreads();
+  uint64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) before += wave_total[i];
+    total += wave_total[i];
   }
+  const float u = v.u[static_cast<size_t>(b) * (v.K + 1) + v.K];
+  const uint32_t r =
+      u > 0.0f ? min(static_cast<uint32_t>(fminf(u, 1.0f) * 16777216.0f), 0xffffffu) : 0u;
+  const uint64_t threshold = (total >> 24) * r + (((total & 0xffffffu) * r) >> 24);
+  if (threshold >= before && threshold < before + s) {
+    uint64_t left = threshold - before;
+    int i = i0;
+    for (; i + 1 < i1; ++i) {
+      const uint64_t w = sum_of(i);
+      if (left < w) break;
+      left -= w;
+    }
+    found_piece = i;
+    found_left = left;
+  }
+  __syncthreads();
+  if (wave == 0 && found_piece >= 0) {
+    if (refused) draw_in_piece<T, true>(v, p, q, found_piece, found_left, &next);
+    else draw_in_piece<T, false>(v, p, q, found_piece, found_left, &next);
+  }
+  __syncthreads();
   if (t == 0) v.accepted[b] = a;
   for (int i = t; i <= v.K; i += kThreads)
     v.out[static_cast<size_t>(b) * (v.K + 1) + i] =
         i < a ? v.tokens[static_cast<size_t>(b) * v.K + i] : (i == a ? next : -1);
 }
+
+// Pieces of a wave: as few as let every workgroup be on the device at once (8
+// of 256 threads on each of 256 CUs), since each first follows the chain of
+// dependent loads to its row.
+constexpr int kWorkgroups = 2048;
+
+template <typename T>
+void launch(VerifyParams v, int B, hipStream_t s) {
+  v.pieces = (v.V + 64 * vec<T>() - 1) / (64 * vec<T>());
+  const int64_t waves = static_cast<int64_t>(v.pieces) * B;
+  const int64_t steps = (waves + kWorkgroups * kWaves - 1) / (kWorkgroups * kWaves);
+  v.steps = static_cast<int32_t>(steps < v.pieces ? steps : v.pieces);
+  const int blocks = (v.pieces + kWaves * v.steps - 1) / (kWaves * v.steps);
+  hipLaunchKernelGGL(verify_kernel<T>, dim3(blocks, B), dim3(kThreads), 0, s, v);
+}
+
+// Tickets have one place whatever B is: a workspace may serve any batch.
+constexpr size_t kTicketBytes = 65536 * sizeof(uint32_t);
 
 }  // namespace
 }  // namespace damp
@@ -169,8 +313,8 @@ extern "C" {
 
 size_t damp_verify_workspace_bytes(int32_t B, int32_t V) {
   if (B <= 0 || B > 65535 || V <= 0 || V > (1 << 22)) return 0;
-  const size_t tiles = (static_cast<size_t>(V) + damp::kTile - 1) / damp::kTile;
-  return static_cast<size_t>(B) * tiles * sizeof(uint64_t);
+  const size_t pieces = (static_cast<size_t>(V) + 255) / 256;
+  return damp::kTicketBytes + static_cast<size_t>(B) * pieces * sizeof(uint64_t);
 }
 
 damp_status damp_verify_drafts(const void* p, const void* q, int32_t dtype, const int32_t* tokens,
@@ -190,6 +334,9 @@ damp_status damp_verify_drafts(const void* p, const void* q, int32_t dtype, cons
   if (B == 0) return DAMP_OK;
   if (!p || !u || !accepted || !out || (K > 0 && (!q || !tokens)))
     return fail(DAMP_ERR_INVALID_ARG, "%s: a required pointer is NULL", name);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q);
+  if (at % (dtype == DAMP_DT_FP32 ? 4 : 2) != 0)
+    return fail(DAMP_ERR_INVALID_ARG, "%s: p and q must be aligned to their type", name);
   const size_t need = damp_verify_workspace_bytes(B, V);
   if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
     return fail(DAMP_ERR_INVALID_ARG, "%s: needs %zu bytes of 16-byte aligned workspace", name,
@@ -202,18 +349,12 @@ damp_status damp_verify_drafts(const void* p, const void* q, int32_t dtype, cons
   v.u = u;
   v.accepted = accepted;
   v.out = out;
-  v.sums = static_cast<uint64_t*>(workspace);
+  v.tickets = static_cast<uint32_t*>(workspace);
+  v.sums = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + kTicketBytes);
   v.K = K;
   v.V = V;
-  v.tiles = (V + kTile - 1) / kTile;
-  hipStream_t s = as_stream(stream);
-  if (dtype == DAMP_DT_FP32) {
-    hipLaunchKernelGGL(verify_sums<float>, dim3(v.tiles, B), dim3(kThreads), 0, s, v);
-    hipLaunchKernelGGL(verify_draw<float>, dim3(B), dim3(kThreads), 0, s, v);
-  } else {
-    hipLaunchKernelGGL(verify_sums<uint16_t>, dim3(v.tiles, B), dim3(kThreads), 0, s, v);
-    hipLaunchKernelGGL(verify_draw<uint16_t>, dim3(B), dim3(kThreads), 0, s, v);
-  }
+  if (dtype == DAMP_DT_FP32) launch<float>(v, B, as_stream(stream));
+  else launch<uint16_t>(v, B, as_stream(stream));
   return check_launch(name);
 }
 

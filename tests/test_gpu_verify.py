@@ -63,8 +63,9 @@ def test_lengths():
 def test_a_workspace_serves_call_after_call():
     print("verify workspace", flush=True)
     ws = torch.zeros(S.damp_verify_workspace_bytes(6, 20001), dtype=torch.uint8, device="cuda")
-    for seed in range(4):
-        check(*case(seed, 6, 4, 20001), ws=ws)
+    for seed, (B, V) in enumerate([(6, 20001), (1, 20001), (6, 300), (3, 9000), (6, 20001)]):
+        check(*case(seed, B, 4, V), ws=ws)
+        assert not bool(ws[:1 << 18].any())
 
 
 def test_drawn_numbers_at_their_ends():
