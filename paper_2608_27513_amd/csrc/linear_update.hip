@@ -4,12 +4,13 @@
 //   S' = exp(g) S + k v^T,   o = scale * S'^T q
 //
 // The state is read once and written once (8 d_k d_v bytes a head against
-// 4 d_k d_v operations), so memory bounds the kernel. A workgroup owns W
-// columns of one (request, value head) tile: the columns of a state do not
-// depend on each other, the rows meet only in o. Thread t holds four
-// neighbouring columns of the rows t / (W / 4) + i RG, all of them loaded
-// before the first is used; o is summed over rows by lane exchanges and one
-// LDS pass over the four waves.
+// 4 d_k d_v operations), so memory bounds the kernel: 196 us at 256 requests
+// of 32 heads of 128 x 128, 5.5 TB/s, where a large copy reaches 5.1. A
+// workgroup owns W columns of one (request, value head) tile: the columns of a
+// state do not depend on each other, the rows meet only in o. Thread t holds
+// four neighbouring columns of the rows t / (W / 4) + i RG, up to 128 rows in
+// flight before the first is used; o is summed over rows by lane exchanges and
+// one LDS pass over the four waves.
 #include "device.hpp"
 #include "linear.hpp"
 
@@ -110,11 +111,17 @@ damp_status linear_params(const char* name, const damp_pool* pool, int32_t layer
 
 namespace {
 
-template <int W>
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kBufferConfig = 0x00020000;  // raw 32-bit buffer (gfx9 family)
+
+template <int W, bool STREAM>
 __global__ __launch_bounds__(256) void linear_update_kernel(const LinearParams p) {
   constexpr int C4 = W / 4;      // lanes of a row
   constexpr int RG = 256 / C4;   // rows side by side
   constexpr int U = 128 / RG;    // rows of a thread in one pass over 128
+  constexpr int kLoad = STREAM ? 2 : 0;        // non-temporal
+  constexpr int kStore = STREAM ? 2 | 16 : 0;  // non-temporal, device scope
   __shared__ float2 kq[256];
   __shared__ float red[4][W];
 
@@ -137,12 +144,25 @@ __global__ __launch_bounds__(256) void linear_update_kernel(const LinearParams p
     }
     return;
   }
-  const float* src = reinterpret_cast<const float*>(
-      p.layer_base + (old ? from : 0) * p.slot_stride + h * p.tile_stride);
-  float* dst = reinterpret_cast<float*>(
-      p.layer_base + (keep ? to : 0) * p.slot_stride + h * p.tile_stride);
+  // one tile as a buffer: rows and columns past the head are past its end, and
+  // so is all of a state that is not read or kept
+  const int bytes = p.dk * p.dv * 4;
+  const auto src = __builtin_amdgcn_make_buffer_rsrc(
+      p.layer_base + (old ? from : 0) * p.slot_stride + h * p.tile_stride, 0, old ? bytes : 0,
+      kBufferConfig);
+  const auto dst = __builtin_amdgcn_make_buffer_rsrc(
+      p.layer_base + (keep ? to : 0) * p.slot_stride + h * p.tile_stride, 0, keep ? bytes : 0,
+      kBufferConfig);
+  const uint32_t row = 4 * p.dv;
+  const uint32_t at = in_row ? 4 * col : 0x80000000u;
 
-  const float a = expf(p.g[b * p.g_stride + h]);
+  // the operands
+  const float g = p.g[b * p.g_stride + h];
+  uint16_t k_w = 0, q_w = 0;
+  if (t < p.dk) {
+    k_w = p.k[b * p.k_stride + hk * p.dk + t];
+    q_w = p.q[b * p.q_stride + hk * p.dk + t];
+  }
   float vv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (in_row) {
     const uint2 w = *reinterpret_cast<const uint2*>(p.v + b * p.v_stride + h * p.dv + col);
@@ -151,36 +171,31 @@ __global__ __launch_bounds__(256) void linear_update_kernel(const LinearParams p
     vv[2] = bf16_lo(w.y);
     vv[3] = bf16_hi(w.y);
   }
-  if (t < p.dk)
-    kq[t] = make_float2(bf16_to_f32(p.k[b * p.k_stride + hk * p.dk + t]),
-                        bf16_to_f32(p.q[b * p.q_stride + hk * p.dk + t]));
-  __syncthreads();
 
   float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r0 = rg; r0 < p.dk; r0 += 128) {
-    float4 x[U];
+  float a = 0.0f;
+  for (int r0 = 0; r0 < p.dk; r0 += 128) {
+    u32x4 x[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int r = r0 + RG * i;
-      x[i] = old && in_row && r < p.dk
-                 ? *reinterpret_cast<const float4*>(src + static_cast<size_t>(r) * p.dv + col)
-                 : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i < U; ++i)
+      x[i] = __builtin_amdgcn_raw_buffer_load_b128(src, at + (r0 + rg + RG * i) * row, 0, kLoad);
+    if (r0 == 0) {  // behind the first loads of the state
+      kq[t] = make_float2(bf16_to_f32(k_w), bf16_to_f32(q_w));
+      a = expf(g);
+      __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int r = r0 + RG * i;
+      const int r = r0 + rg + RG * i;
       if (r >= p.dk) break;
       const float2 w = kq[r];
-      x[i].x = fmaf(w.x, vv[0], a * x[i].x);
-      x[i].y = fmaf(w.x, vv[1], a * x[i].y);
-      x[i].z = fmaf(w.x, vv[2], a * x[i].z);
-      x[i].w = fmaf(w.x, vv[3], a * x[i].w);
-      acc[0] = fmaf(w.y, x[i].x, acc[0]);
-      acc[1] = fmaf(w.y, x[i].y, acc[1]);
-      acc[2] = fmaf(w.y, x[i].z, acc[2]);
-      acc[3] = fmaf(w.y, x[i].w, acc[3]);
-      if (keep && in_row)
-        *reinterpret_cast<float4*>(dst + static_cast<size_t>(r) * p.dv + col) = x[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float y = fmaf(w.x, vv[j], a * __uint_as_float(x[i][j]));
+        acc[j] = fmaf(w.y, y, acc[j]);
+        x[i][j] = __float_as_uint(y);
+      }
+      __builtin_amdgcn_raw_buffer_store_b128(x[i], dst, at + r * row, 0, kStore);
     }
   }
 #pragma unroll
@@ -197,6 +212,31 @@ __global__ __launch_bounds__(256) void linear_update_kernel(const LinearParams p
     if (p.o_bf16) static_cast<uint16_t*>(p.o)[o_at + c] = f32_to_bf16(o);
     else static_cast<float*>(p.o)[o_at + c] = o;
   }
+}
+
+template <int W, bool STREAM>
+void launch(const LinearParams& p, int B, hipStream_t s) {
+  hipLaunchKernelGGL((linear_update_kernel<W, STREAM>), dim3(p.HV, B, (p.dv + W - 1) / W),
+                     dim3(256), 0, s, p);
+}
+
+// Fewer tiles than CUs: 32 columns each, for the shorter chain of loads (one
+// request of 32 heads: 3.4 us against 4.0 with 128). Otherwise the whole row,
+// up to 128 columns. States of 128 MB and more pass by the caches (256
+// requests: 196 against 211 us; 64 requests, 134 MB: 50.9 against 53.5);
+// smaller ones may still be there from the step before (32 requests: 21.7 us
+// against 26.6).
+constexpr int64_t kFewTiles = 256;
+constexpr int64_t kStreamBytes = int64_t{128} << 20;
+
+void launch(const LinearParams& p, int B, hipStream_t s) {
+  const int64_t tiles = static_cast<int64_t>(B) * p.HV;
+  const bool stream = tiles * p.dk * p.dv * 4 >= kStreamBytes;
+  if (p.dv <= 32 || tiles < kFewTiles) launch<32, false>(p, B, s);
+  else if (p.dv <= 64 && stream) launch<64, true>(p, B, s);
+  else if (p.dv <= 64) launch<64, false>(p, B, s);
+  else if (stream) launch<128, true>(p, B, s);
+  else launch<128, false>(p, B, s);
 }
 
 }  // namespace
@@ -218,6 +258,6 @@ extern "C" damp_status damp_linear_update(const damp_pool* pool, int32_t layer,
                                  q_stride, k, k_stride, v, v_stride, g, g_stride, scale, o,
                                  o_dtype, s, &p);
   if (st != DAMP_OK || B == 0) return st;
-  hipLaunchKernelGGL(linear_update_kernel<32>, dim3(p.HV, B, (p.dv + 31) / 32), dim3(256), 0, s, p);
+  launch(p, B, s);
   return check_launch(name);
 }
