@@ -47,6 +47,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
+constexpr int NW = 4;  // waves of a workgroup, 32 columns each
 constexpr int kBufferConfig = 0x00020000;  // raw 32-bit buffer (gfx9 family)
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer here
 constexpr float kLeastLog = -1000.0f;
@@ -64,12 +65,18 @@ struct PromptParams {
   int32_t segments;  // of the longest request
 };
 
+// One number of a request, the same in every lane, and in a scalar register:
+// what buffers are described by has to be.
+__device__ __forceinline__ int of_request(const int32_t* numbers, int b) {
+  return __builtin_amdgcn_readfirstlane(numbers[b]);
+}
+
 // First token and length of request b, within the token axis and max_len.
 __device__ __forceinline__ void request_range(const PromptParams& p, int b, int& start, int& len) {
-  start = p.seq_start[b];
+  start = of_request(p.seq_start, b);
   const bool inside = start >= 0 && start <= p.n_tokens;
-  len = inside ? min(min(p.seq_len[b], p.max_len), p.n_tokens - start) : 0;
-  len = max(len, 0);
+  len = inside ? min(min(of_request(p.seq_len, b), p.max_len), p.n_tokens - start) : 0;
+  len = __builtin_amdgcn_readfirstlane(max(len, 0));
   if (!inside) start = 0;
 }
 
@@ -99,19 +106,6 @@ __device__ __forceinline__ void split8(float (&x)[8], u32x4 (&out)[PARTS]) {
   }
 }
 
-// One pair's next part: its bf16 word, with what it leaves in the pair.
-__device__ __forceinline__ uint32_t next_part(float& a, float& b) {
-  const uint32_t w = pack_bf16x2(a, b);
-  a -= bf16_lo(w);
-  b -= bf16_hi(w);
-  return w;
-}
-
-// Keeps vector and matrix instructions on their sides (loads may pass): a
-// matrix instruction takes 32 cycles of its unit and the six others written
-// after it 4 each of theirs, which run side by side in this order only.
-__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x7f4); }
-
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // Four tokens of one column per lane, from rows of 16-bit values in LDS: each
@@ -130,7 +124,8 @@ __device__ __forceinline__ bf16x8 read_columns8(const uint16_t* at, int step) {
 // give zeros and writes to them are dropped. row_bytes * 64 < 2^31.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* base, int64_t row0,
                                                           int64_t row_bytes, int rows) {
-  const int n = max(min(rows, kChunk), 0);
+  // (a clamp is a vector instruction: back into a scalar register)
+  const int n = __builtin_amdgcn_readfirstlane(max(min(rows, kChunk), 0));
   return __builtin_amdgcn_make_buffer_rsrc(
       const_cast<uint8_t*>(static_cast<const uint8_t*>(base)) + row0 * row_bytes, 0,
       n * static_cast<int>(row_bytes), kBufferConfig);
@@ -165,7 +160,7 @@ __device__ __forceinline__ double wave_scan_f64(double x) {
 // PARTS = 0: the first pass, which leaves the state of each segment but the
 // last from a zero start. PARTS = 2 or 3: outputs, with so many parts of S
 // and P.
-template <int DK, int NW, int PARTS>
+template <int DK, int PARTS>
 __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(const PromptParams pp) {
   const LinearParams& p = pp.l;
   constexpr bool kOut = PARTS > 0;
@@ -188,7 +183,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   __shared__ float from_start[2][kChunk];  // times the scale
   __shared__ float chunk_decay[2];
 
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int half = lane >> 5, n32 = lane & 31;
   const int blocks_v = (p.dv + 32 * NW - 1) / (32 * NW);
   const int nx = p.HV * blocks_v;
@@ -205,7 +200,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   const int64_t tok0 = static_cast<int64_t>(start) + static_cast<int64_t>(seg) * pp.seg_len;
   const int count = min(pp.seg_len, len - seg * pp.seg_len);
 
-  const int from = p.slot_in[b], to = p.slot_out[b];
+  const int from = of_request(p.slot_in, b), to = of_request(p.slot_out, b);
   const bool old = from >= 0 && from < p.num_slots;
   const bool keep = to >= 0 && to < p.num_slots;
   if (!old && from != DAMP_SLOT_ZERO) {  // padded request
@@ -332,7 +327,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     // (past the end the buffers are empty and their loads give zeros)
     const Rows next = rows(kChunk);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(next, i);
+    for (int i = 0; i < (kOut ? KV : kLoads); ++i) load(next, i);
   }
   for (int first = 0; first < count; first += kChunk) {
     const int buf = (first / kChunk) & 1;
@@ -340,10 +335,13 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     __syncthreads();  // the chunk is there
 
     const float all = chunk_decay[buf];
+    const bool whole = PARTS != 2 || (seg == segs - 1 && keep);
     f32x16 O[2];
     if constexpr (kOut) {
+      const Rows soon = rows(first + kChunk);
       // ---- scores of tiles (tokens j, tokens i): (0, 0), (0, 1), (1, 1)
-      for (int w = wave; w < 3; w += NW) {
+      if (wave < 3) {
+        const int w = wave;
         const int jt = w >> 1, it = (w + 1) >> 1;
         f32x16 A;
 #pragma unroll
@@ -380,40 +378,23 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       for (int it = 0; it < 2; ++it)
 #pragma unroll
         for (int r = 0; r < 16; ++r) O[it][r] = 0.0f;
-      u32x4 part[2][NP];  // of this step's eight rows and of the next
-      {
+#pragma unroll
+      for (int e = 0; e < 2 * KT; ++e) {  // 16 channels each; Q and V of the next chunk on the way
+#pragma unroll
+        for (int i = KV + e * (KV + VV) / (2 * KT); i < KV + (e + 1) * (KV + VV) / (2 * KT); ++i)
+          load(soon, i);
         float y[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) y[r] = S[0][r];
-        split8<NP>(y, part[0]);
-      }
-      auto q_rows = [&](int it, int e) {
-        return *reinterpret_cast<const bf16x8*>(qt + (32 * it + n32) * QS + 16 * e + 8 * half);
-      };
-      bf16x8 qa[2][2] = {{q_rows(0, 0), q_rows(1, 0)}};
+        for (int r = 0; r < 8; ++r) y[r] = S[e / 2][8 * (e % 2) + r];
+        u32x4 part[NP];
+        split8<NP>(y, part);
 #pragma unroll
-      for (int e = 0; e < 2 * KT; ++e) {
-        if (e + 1 < 2 * KT)
+        for (int it = 0; it < 2; ++it) {
+          const bf16x8 qa =
+              *reinterpret_cast<const bf16x8*>(qt + (32 * it + n32) * QS + 16 * e + 8 * half);
 #pragma unroll
-          for (int it = 0; it < 2; ++it) qa[(e + 1) % 2][it] = q_rows(it, e + 1);
-        float y[8];
-        if (e + 1 < 2 * KT)
-#pragma unroll
-          for (int r = 0; r < 8; ++r) y[r] = S[(e + 1) / 2][8 * ((e + 1) % 2) + r];
-        // the next step's parts, and this one's rows decayed, between the products
-#pragma unroll
-        for (int m = 0; m < 2 * NP; ++m) {
-          const int it = m % 2, n = m / 2;
-          O[it] = mfma(__builtin_bit_cast(bf16x8, part[e % 2][n]), qa[e % 2][it], O[it]);
-          if (e + 1 < 2 * KT) {
-#pragma unroll
-            for (int i = m * 4 * NP / (2 * NP); i < (m + 1) * 4 * NP / (2 * NP); ++i)
-              part[(e + 1) % 2][i / 4][i % 4] = next_part(y[2 * (i % 4)], y[2 * (i % 4) + 1]);
-          }
-#pragma unroll
-          for (int i = m * 8 / (2 * NP); i < (m + 1) * 8 / (2 * NP); ++i)
-            S[e / 2][8 * (e % 2) + i] *= all;
-          keep_order();
+          for (int n = 0; n < NP; ++n)
+            O[it] = mfma(__builtin_bit_cast(bf16x8, part[n]), qa, O[it]);
         }
       }
 #pragma unroll
@@ -434,52 +415,27 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     // ---- S = exp(L_C) S + K^T (D V)
     // the state's row order: the quads of 16 channels as 0 2 1 3
     const int k_quad = 4 * (((lane & 1) << 1) | ((lane >> 1) & 1));
-    auto scaled = [&](int s, int i, float& a, float& b) {  // D V of 2 of the 8 tokens
-      const float2 d = *reinterpret_cast<const float2*>(to_end[buf] + 16 * s + 8 * (i / 2) +
-                                                        4 * half + 2 * (i % 2));
-      const uint32_t w = __builtin_bit_cast(u32x4, va[s])[i];
-      a = bf16_lo(w) * d.x;
-      b = bf16_hi(w) * d.y;
-    };
-    auto k_columns = [&](int s, int c) {
-      return read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
-    };
-    bf16x8 ka[2] = {k_columns(0, 0)};
-    if constexpr (!kOut)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) S[0][r] *= all;
-    u32x4 dv[2][3];
+    for (int c = 0; c < KT; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float a, b;
-      scaled(0, i, a, b);
-#pragma unroll
-      for (int n = 0; n < 3; ++n) dv[0][n][i] = next_part(a, b);
-    }
+      for (int r = 0; r < 16; ++r) S[c][r] *= all;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      float a = 0.0f, b = 0.0f;
+      const float4 d0 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half);
+      const float4 d1 = *reinterpret_cast<const float4*>(to_end[buf] + 16 * s + 4 * half + 8);
+      const u32x4 w = __builtin_bit_cast(u32x4, va[s]);
+      float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
+                    bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
+                    bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
+      u32x4 part[3];
+      split8<3>(y, part);
 #pragma unroll
       for (int c = 0; c < KT; ++c) {
-        const int next = s * KT + c + 1;
-        if (next < 4 * KT) ka[next % 2] = k_columns(next / KT, next % KT);
-#pragma unroll
-        for (int n = 0; n < 3; ++n) {
-          S[c] = mfma(ka[(next - 1) % 2], __builtin_bit_cast(bf16x8, dv[s % 2][n]), S[c]);
-          // the next step's parts between this one's products
-          if (s < 3) {
-            const int m = 3 * c + n;
-#pragma unroll
-            for (int i = m * 4 / KT; i < (m + 1) * 4 / KT; ++i) {  // 12 steps over 3 KT products
-              if (i % 3 == 0) scaled(s + 1, i / 3, a, b);
-              dv[(s + 1) % 2][i % 3][i / 3] = next_part(a, b);
-            }
-          }
-          if (!kOut && s == 0 && c + 1 < KT)
-#pragma unroll
-            for (int r = n * 16 / 3; r < (n + 1) * 16 / 3; ++r) S[c + 1][r] *= all;
-          keep_order();
-        }
+        const bf16x8 ka =
+            read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
+        S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[0]), S[c]);
+        S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[1]), S[c]);
+        if (whole) S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[2]), S[c]);
       }
     }
 
@@ -504,8 +460,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
         O[it] = mfma(va[s], __builtin_bit_cast(bf16x8, pt[((w * 2 + (s & 1)) * NP + n) * 64 + lane]),
                      O[it]);
 #pragma unroll
-        for (int i = m * kLoads / (6 * NP); i < (m + 1) * kLoads / (6 * NP); ++i) load(ahead, i);
-        __builtin_amdgcn_sched_barrier(0x786);  // LDS, scalar and vector only may pass
+        for (int i = m * KV / (6 * NP); i < (m + 1) * KV / (6 * NP); ++i) load(ahead, i);
       }
       const auto obuf = rows_of(static_cast<uint8_t*>(p.o) + (static_cast<int64_t>(h) * p.dv + col0) *
                                                                  (p.o_bf16 ? 2 : 4),
@@ -602,14 +557,16 @@ __global__ __launch_bounds__(256) void prompt_states(const PromptParams pp) {
 
 // Tokens of a segment. The lengths are on the device; the host knows that B
 // requests share n_tokens and none is longer than max_len. Segments are as
-// long as leave every CU its two workgroups, at least kLeastSegment tokens,
+// long as leave every CU its two workgroups, at least kLeastSegment tokens (a
+// request of up to kUncut is not cut: the two other launches would cost more),
 // and no shorter than the finest cut, which goes by B and max_len alone and
 // which the workspace has room for. Measured on 256 CUs, in us: one request of
 // 32768 tokens and 32 heads in 512 / 1024 / 2048 / 4096 pieces 391 / 416 / 444
-// / 522; eleven of 1 to 4096 tokens in 240 / 490 / 970: 214 / 155 / 157.
+// / 522; eleven of 1 to 4096 tokens in 240 / 490 / 970: 214 / 155 / 157; one
+// of 200 whole 22, in two 27; one of 500 in segments of 128 / 256: 30 / 40.
 constexpr int kWorkgroups = 512;
 constexpr int kMostWorkgroups = 4096;
-constexpr int kLeastSegment = 256;
+constexpr int kLeastSegment = 128, kUncut = 256;
 
 struct Split {
   int32_t seg_len, segments;
@@ -621,7 +578,9 @@ Split split_of(const damp_pool* pool, int32_t B, int64_t n_tokens, int32_t max_l
   const int64_t finest = (longest * B * heads + kMostWorkgroups - 1) / kMostWorkgroups;
   const int64_t wanted = ((n_tokens / kChunk + B) * heads + kWorkgroups - 1) / kWorkgroups;
   const int64_t seg = std::min<int64_t>(
-      std::max<int64_t>({finest * kChunk, wanted * kChunk, kLeastSegment}), 1 << 30);
+      std::max<int64_t>({finest * kChunk, wanted * kChunk,
+                         max_len <= kUncut ? kUncut : kLeastSegment}),
+      1 << 30);
   return {static_cast<int32_t>(seg),
           static_cast<int32_t>(std::max<int64_t>((max_len + seg - 1) / seg, 1))};
 }
@@ -632,25 +591,19 @@ size_t workspace_bytes_of(const damp_pool* pool, int32_t B, const Split& s) {
   return tiles * (static_cast<size_t>(pool->layout.d_k) * pool->layout.d_v + 1) * sizeof(float);
 }
 
-template <int DK, int NW>
+template <int DK>
 void launch(const PromptParams& p, int B, hipStream_t s) {
   const int nx = p.l.HV * ((p.l.dv + 32 * NW - 1) / (32 * NW));
   if (p.segments > 1) {
-    hipLaunchKernelGGL((prompt_chunks<DK, NW, 0>), dim3(nx, B, p.segments - 1), dim3(64 * NW), 0, s,
+    hipLaunchKernelGGL((prompt_chunks<DK, 0>), dim3(nx, B, p.segments - 1), dim3(64 * NW), 0, s,
                        p);
     hipLaunchKernelGGL(prompt_states, dim3(p.l.HV, B, (p.l.dk * p.l.dv + 1023) / 1024), dim3(256),
                        0, s, p);
   }
   if (p.l.o_bf16)
-    hipLaunchKernelGGL((prompt_chunks<DK, NW, 2>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+    hipLaunchKernelGGL((prompt_chunks<DK, 2>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
   else
-    hipLaunchKernelGGL((prompt_chunks<DK, NW, 3>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
-}
-
-template <int DK>
-void launch_dk(const PromptParams& p, int B, hipStream_t s) {
-  if (p.l.dv <= 64) launch<DK, 2>(p, B, s);
-  else launch<DK, 4>(p, B, s);
+    hipLaunchKernelGGL((prompt_chunks<DK, 3>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
 }
 
 }  // namespace
@@ -708,9 +661,9 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
   p.segments = split.segments;
   p.seg_states = static_cast<float*>(workspace);
   p.seg_decays = p.seg_states + static_cast<size_t>(B) * split.segments * p.l.HV * p.l.dk * p.l.dv;
-  if (p.l.dk <= 64) launch_dk<64>(p, B, s);
-  else if (p.l.dk <= 128) launch_dk<128>(p, B, s);
-  else launch_dk<256>(p, B, s);
+  if (p.l.dk <= 64) launch<64>(p, B, s);
+  else if (p.l.dk <= 128) launch<128>(p, B, s);
+  else launch<256>(p, B, s);
   return check_launch(name);
 }
 

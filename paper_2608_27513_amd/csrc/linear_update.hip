@@ -131,7 +131,9 @@ __global__ __launch_bounds__(256) void linear_update_kernel(const LinearParams p
   const int col = blockIdx.z * W + 4 * cg;
   const bool in_row = col < p.dv;
   const int hk = h / (p.HV / p.HK);
-  const int from = p.slot_in[b], to = p.slot_out[b];
+  // in scalar registers, as what buffers are described by has to be
+  const int from = __builtin_amdgcn_readfirstlane(p.slot_in[b]);
+  const int to = __builtin_amdgcn_readfirstlane(p.slot_out[b]);
   const bool old = from >= 0 && from < p.num_slots;
   const bool keep = to >= 0 && to < p.num_slots;
   const size_t o_at = (static_cast<size_t>(b) * p.HV + h) * p.dv;
