@@ -88,7 +88,8 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// Eight values as PARTS bf16 vectors that add up to them.
+// Eight values as PARTS bf16 vectors that add up to them; x keeps what the last
+// part was rounded from.
 template <int PARTS>
 __device__ __forceinline__ void split8(float (&x)[8], u32x4 (&out)[PARTS]) {
 #pragma unroll
@@ -427,15 +428,25 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       float y[8] = {bf16_lo(w[0]) * d0.x, bf16_hi(w[0]) * d0.y, bf16_lo(w[1]) * d0.z,
                     bf16_hi(w[1]) * d0.w, bf16_lo(w[2]) * d1.x, bf16_hi(w[2]) * d1.y,
                     bf16_lo(w[3]) * d1.z, bf16_hi(w[3]) * d1.w};
-      u32x4 part[3];
-      split8<3>(y, part);
+      auto k_columns = [&](int c) {
+        return read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
+      };
+      u32x4 part[2];
+      split8<2>(y, part);
 #pragma unroll
       for (int c = 0; c < KT; ++c) {
-        const bf16x8 ka =
-            read_columns8(kt + (16 * s + tr_row) * KS + 32 * c + tr_col + k_quad, 8 * KS);
-        S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[0]), S[c]);
-        S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[1]), S[c]);
-        if (whole) S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[2]), S[c]);
+        const bf16x8 ka = k_columns(c);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) S[c] = mfma(ka, __builtin_bit_cast(bf16x8, part[n]), S[c]);
+      }
+      if (whole) {
+        u32x4 third;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          third[j] = pack_bf16x2(y[2 * j] - bf16_lo(part[1][j]), y[2 * j + 1] - bf16_hi(part[1][j]));
+#pragma unroll
+        for (int c = 0; c < KT; ++c)
+          S[c] = mfma(k_columns(c), __builtin_bit_cast(bf16x8, third), S[c]);
       }
     }
 

@@ -190,6 +190,20 @@ def test_prompt_sizes(dk, dv, o_type):
     run_prompts(x, lens, [0, 4, 2, -1, 1], [0, 4, 2, 3, 5], o_type=o_type)
 
 
+@pytest.mark.parametrize("dk,dv", [(256, 64), (160, 128), (136, 32), (256, 256), (248, 200)])
+@pytest.mark.parametrize("o_type", [torch.float32, torch.bfloat16])
+def test_prompt_wide_keys(dk, dv, o_type):
+    """Keys of more than 128 channels, whose states take most of a wave's
+    registers: one chunk and several, from zero states and old ones, whole and
+    in segments."""
+    print(f"prompt wide {dk}x{dv} {o_type}", flush=True)
+    for seed, lens in enumerate([[20], [64], [65, 190], [700]]):
+        B = len(lens)
+        x = Setup(40 + seed, sum(lens), 2, 1, dk, dv, 2 * B)
+        run_prompts(x, lens, [-1 if seed % 2 else 2 * b for b in range(B)],
+                    [2 * b + 1 for b in range(B)], o_type=o_type)
+
+
 @pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257,
                                1000])
 def test_prompt_lengths(T):
