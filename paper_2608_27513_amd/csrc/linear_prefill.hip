@@ -28,6 +28,16 @@
 // good to fp32 however far the sum has run. A log-decay below -1000 counts as
 // that (its factor is 0 in fp32 either way), so -inf makes no inf - inf.
 //
+// q, k, v and o set the floor: memory, as 4 d_k d_v operations a token and head
+// are few beside their bytes. What bounds the kernel is the issue of vector and matrix
+// instructions and the waits between them: at 32768 tokens, 32 heads of 128 and
+// o in bf16, three launches of 128 + 12 + 234 us, 187 TFLOP/s of the recurrence's
+// operations and 2.2 TB/s of the floor's bytes, the third launch with its matrix
+// units busy 37% and its vector issue 41% of the time, two waves a SIMD. Tried
+// and not kept: the parts of the next step placed between the products of this
+// one (the same time), 2 waves and 64 columns a workgroup (2% faster at d_v = 64,
+// slower at 128), a fourth wave that repeats a score tile to avoid the branch.
+//
 // Where there are fewer requests and heads than the device has room for, the
 // tokens are cut into segments: a first pass leaves the state that each
 // segment adds, a second runs over the segments to the state before each,
