@@ -58,6 +58,10 @@ extern "C" {
  * in elements (a multiple of 8, at least one token's heads; so they may be
  * left where a fused projection wrote them). g fp32 [tokens, HV] with the
  * token distance g_stride >= HV, or g_stride = 0 for one decay a head.
+ * Operands and states must be finite (g may be -inf): a NaN or an infinity
+ * may reach any output of its own request, those of earlier tokens included,
+ * and its state; it reaches no other request, and what lies outside the
+ * requests' tokens is not read.
  * o [tokens, HV, d_v] contiguous in o_dtype (DAMP_DT_FP32 or DAMP_DT_BF16),
  * 16-byte aligned.
  * ---------------------------------------------------------------------- */
@@ -92,8 +96,8 @@ size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B,
  *  workspace  damp_linear_prefill_workspace_bytes(pool, B, max_len) bytes,
  *             16-byte aligned (NULL where that is 0). Calls that may overlap
  *             need one each.
- * B = 0 is a no-op; B <= 65535; n_tokens < 2^31; token distances below 2^24
- * and HV d_v below 2^23 elements. */
+ * B = 0 is a no-op; B <= 65535; n_tokens < 2^31; token distances of at most
+ * 2^24 - 16 and HV d_v of at most 2^23 - 8 elements. */
 damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer,
                                 const int32_t* slot_in, const int32_t* slot_out,
                                 int32_t B, int64_t n_tokens, int32_t max_len,
