@@ -35,8 +35,8 @@
 // operations and 2.2 TB/s of the floor's bytes, the third launch with its matrix
 // units busy 37% and its vector issue 41% of the time, two waves a SIMD. Tried
 // and not kept: the parts of the next step placed between the products of this
-// one (the same time), 2 waves and 64 columns a workgroup (2% faster at d_v = 64,
-// slower at 128), a fourth wave that repeats a score tile to avoid the branch.
+// one (the same time), a fourth wave that repeats a score tile to avoid the
+// branch (slower).
 //
 // Where there are fewer requests and heads than the device has room for, the
 // tokens are cut into segments: a first pass leaves the state that each
@@ -57,7 +57,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;
-constexpr int NW = 4;  // waves of a workgroup, 32 columns each
 constexpr int kBufferConfig = 0x00020000;  // raw 32-bit buffer (gfx9 family)
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer here
 constexpr float kLeastLog = -1000.0f;
@@ -171,7 +170,7 @@ __device__ __forceinline__ double wave_scan_f64(double x) {
 // PARTS = 0: the first pass, which leaves the state of each segment but the
 // last from a zero start. PARTS = 2 or 3: outputs, with so many parts of S
 // and P.
-template <int DK, int PARTS>
+template <int DK, int NW, int PARTS>
 __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(const PromptParams pp) {
   const LinearParams& p = pp.l;
   constexpr bool kOut = PARTS > 0;
@@ -351,8 +350,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     if constexpr (kOut) {
       const Rows soon = rows(first + kChunk);
       // ---- scores of tiles (tokens j, tokens i): (0, 0), (0, 1), (1, 1)
-      if (wave < 3) {
-        const int w = wave;
+      for (int w = wave; w < 3; w += NW) {
         const int jt = w >> 1, it = (w + 1) >> 1;
         f32x16 A;
 #pragma unroll
@@ -612,19 +610,28 @@ size_t workspace_bytes_of(const damp_pool* pool, int32_t B, const Split& s) {
   return tiles * (static_cast<size_t>(pool->layout.d_k) * pool->layout.d_v + 1) * sizeof(float);
 }
 
-template <int DK>
+template <int DK, int NW>
 void launch(const PromptParams& p, int B, hipStream_t s) {
   const int nx = p.l.HV * ((p.l.dv + 32 * NW - 1) / (32 * NW));
   if (p.segments > 1) {
-    hipLaunchKernelGGL((prompt_chunks<DK, 0>), dim3(nx, B, p.segments - 1), dim3(64 * NW), 0, s,
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 0>), dim3(nx, B, p.segments - 1), dim3(64 * NW), 0, s,
                        p);
     hipLaunchKernelGGL(prompt_states, dim3(p.l.HV, B, (p.l.dk * p.l.dv + 1023) / 1024), dim3(256),
                        0, s, p);
   }
   if (p.l.o_bf16)
-    hipLaunchKernelGGL((prompt_chunks<DK, 2>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 2>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
   else
-    hipLaunchKernelGGL((prompt_chunks<DK, 3>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+    hipLaunchKernelGGL((prompt_chunks<DK, NW, 3>), dim3(nx, B, p.segments), dim3(64 * NW), 0, s, p);
+}
+
+// Two waves where the head has no columns for four: 16 requests of 2000 tokens,
+// 32 heads of 64, take 165 us against 170, with keys of 128 channels 195 against
+// 214.
+template <int DK>
+void launch(const PromptParams& p, int B, hipStream_t s) {
+  if (p.l.dv <= 64) launch<DK, 2>(p, B, s);
+  else launch<DK, 4>(p, B, s);
 }
 
 }  // namespace
