@@ -97,7 +97,7 @@ size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B,
  *             16-byte aligned (NULL where that is 0). Calls that may overlap
  *             need one each.
  * B = 0 is a no-op; B <= 65535; n_tokens < 2^31; token distances of at most
- * 2^24 - 16 and HV d_v of at most 2^23 - 8 elements. */
+ * 2^24 - 16 (of g, 2^23 - 8) and HV d_v of at most 2^23 - 8 elements. */
 damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer,
                                 const int32_t* slot_in, const int32_t* slot_out,
                                 int32_t B, int64_t n_tokens, int32_t max_len,

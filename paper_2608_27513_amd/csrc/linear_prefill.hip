@@ -130,6 +130,12 @@ __device__ __forceinline__ bf16x8 read_columns8(const uint16_t* at, int step) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// An offset into a buffer, past its end where `in` is false; as a select.
+__device__ __forceinline__ uint32_t offset_if(bool in, uint32_t at) {
+  asm("" : "+v"(at));
+  return in ? at : kNowhere;
+}
+
 // The rows from `row0` on of a chunk as a buffer: reads of rows past `rows`
 // give zeros and writes to them are dropped. row_bytes * 64 < 2^31.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* base, int64_t row0,
@@ -193,6 +199,10 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   __shared__ float from_start[2][kChunk];  // times the scale
   __shared__ float chunk_decay[2];
 
+  // Branches from here on go by scalars. In a branch that only some lanes or
+  // waves take, the compiler may save a register before the others are back,
+  // which then lose it: seen with states of 256 channels, whose accumulators
+  // crowd the rest out of the vector registers.
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int half = lane >> 5, n32 = lane & 31;
   const int blocks_v = (p.dv + 32 * NW - 1) / (32 * NW);
@@ -237,7 +247,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   // this lane's first row and column; rows and columns past the head are
   // past the buffer's end
   const uint32_t s_row = 4 * p.dv;
-  const uint32_t s_at = col < p.dv ? 8 * half * s_row + 4 * col : kNowhere;
+  const uint32_t s_at = offset_if(col < p.dv, 8 * half * s_row + 4 * col);
   f32x16 S[KT];
 #pragma unroll
   for (int c = 0; c < KT; ++c)
@@ -265,10 +275,12 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   const int64_t o_row = static_cast<int64_t>(p.HV) * p.dv * (p.o_bf16 ? 2 : 4);
   constexpr int kRows = NT / (DK / 8), vRows = 16;  // rows that one load instruction spans
   const int k8 = t % (DK / 8), v8 = t % (4 * NW);
-  const uint32_t k_at = 8 * k8 < p.dk ? t / (DK / 8) * static_cast<uint32_t>(k_row) + 16 * k8 : kNowhere;
-  const uint32_t q_at = 8 * k8 < p.dk ? t / (DK / 8) * static_cast<uint32_t>(q_row) + 16 * k8 : kNowhere;
-  const uint32_t v_at = col0 + 8 * v8 < p.dv ? t / (4 * NW) * static_cast<uint32_t>(v_row) + 16 * v8
-                                             : kNowhere;
+  const uint32_t k_at =
+      offset_if(8 * k8 < p.dk, t / (DK / 8) * static_cast<uint32_t>(k_row) + 16 * k8);
+  const uint32_t q_at =
+      offset_if(8 * k8 < p.dk, t / (DK / 8) * static_cast<uint32_t>(q_row) + 16 * k8);
+  const uint32_t v_at =
+      offset_if(col0 + 8 * v8 < p.dv, t / (4 * NW) * static_cast<uint32_t>(v_row) + 16 * v8);
   u32x4 kr[KV], qr[kOut ? KV : 1], vr[VV];
   // load i of a thread: K, Q, then V
   constexpr int kLoads = (kOut ? 2 : 1) * KV + VV;
@@ -298,8 +310,15 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   const bool decays = wave == NW - 1;
   float gr = 0.0f;
   double run_log = 0.0;  // of the segment so far
+  const int64_t g_row = 4 * p.g_stride;
   auto load_g = [&](int first) {
-    gr = first + lane < count ? gb[(tok0 + first + lane) * p.g_stride] : 0.0f;
+    // one decay a head is a row of no length: its buffer ends behind the number
+    const int rows = __builtin_amdgcn_readfirstlane(max(min(count - first, kChunk), 0));
+    const auto gbuf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(gb)) + (tok0 + first) * g_row, 0,
+        rows > 0 ? (rows - 1) * static_cast<int>(g_row) + 4 : 0, kBufferConfig);
+    gr = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+        gbuf, offset_if(lane < rows, lane * static_cast<uint32_t>(g_row)), 0, 0));
   };
   auto scan_g = [&](int to_buf) {
     const double s = wave_scan_f64(static_cast<double>(gr < kLeastLog ? kLeastLog : gr) * kLog2e);
@@ -309,7 +328,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     logs[to_buf][lane] = make_float2(static_cast<float>(coarse), static_cast<float>(s - coarse));
     to_end[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(all - s));
     from_start[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(s)) * p.scale;
-    if (lane == 0) chunk_decay[to_buf] = __builtin_amdgcn_exp2f(static_cast<float>(all));
+    chunk_decay[to_buf] = __builtin_amdgcn_exp2f(static_cast<float>(all));
   };
 
   auto stage = [&] {
@@ -503,7 +522,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
               w[2 + e] = x[1];
             }
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, obuf, col0 + c < p.dv ? row_at + 2 * c : kNowhere, 0, 0);
+                w, obuf, offset_if(col0 + c < p.dv, row_at + 2 * c), 0, 0);
           }
         } else {
 #pragma unroll
@@ -512,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
             const u32x4 w = {__float_as_uint(y[4 * r4]), __float_as_uint(y[4 * r4 + 1]),
                              __float_as_uint(y[4 * r4 + 2]), __float_as_uint(y[4 * r4 + 3])};
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, obuf, col0 + c < p.dv ? row_at + 4 * c : kNowhere, 0, 0);
+                w, obuf, offset_if(col0 + c < p.dv, row_at + 4 * c), 0, 0);
           }
         }
       }
@@ -526,7 +545,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       dst = reinterpret_cast<float*>(p.layer_base + to * p.slot_stride + h * p.tile_stride);
   } else {
     dst = pp.seg_states + tile + seg * tile_step;
-    if (decays && lane == 0 && col0 == 0)
+    if (decays && col0 == 0)
       pp.seg_decays[(static_cast<size_t>(b) * pp.segments + seg) * p.HV + h] =
           __builtin_amdgcn_exp2f(static_cast<float>(run_log));
   }
@@ -672,7 +691,7 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
   if (st != DAMP_OK || B == 0) return st;
   // a chunk's rows are addressed with 31 bits
   constexpr int64_t kMost = (int64_t{1} << 31) / kChunk / 4 - 8;
-  if (q_stride > 2 * kMost || k_stride > 2 * kMost || v_stride > 2 * kMost ||
+  if (q_stride > 2 * kMost || k_stride > 2 * kMost || v_stride > 2 * kMost || g_stride > kMost ||
       static_cast<int64_t>(p.l.HV) * p.l.dv > kMost)
     return fail(DAMP_ERR_INVALID_ARG, "%s: a token's row is too long", name);
   const Split split = split_of(pool, B, n_tokens, max_len);
