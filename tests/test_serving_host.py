@@ -87,6 +87,11 @@ def test_linear_refusals(L):
     a = list(pre)
     a[4] = 0
     assert L.damp_linear_prefill(*a) == D.DAMP_OK
+    for i, val in ((11, 2 ** 24), (13, 2 ** 24), (15, 2 ** 24), (17, 2 ** 23)):
+        a = list(pre)  # rows whose chunk does not fit 31 bits
+        a[i] = val
+        st, msg = status(L.damp_linear_prefill, *a)
+        assert st == D.DAMP_ERR_INVALID_ARG and "too long" in msg, i
     for bad in (pool_of(kind=D.DAMP_STATE_MIXED), pool_of(dk=60), pool_of(dv=264), pool_of(dv=4)):
         st, msg = status(L.damp_linear_update, ctypes.byref(bad), *up[1:])
         assert st == D.DAMP_ERR_UNSUPPORTED and "multiples of 8" in msg
