@@ -522,7 +522,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
               w[2 + e] = x[1];
             }
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, obuf, offset_if(col0 + c < p.dv, row_at + 2 * c), 0, 0);
+                w, obuf, col0 + c < p.dv ? row_at + 2 * c : kNowhere, 0, 0);
           }
         } else {
 #pragma unroll
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
             const u32x4 w = {__float_as_uint(y[4 * r4]), __float_as_uint(y[4 * r4 + 1]),
                              __float_as_uint(y[4 * r4 + 2]), __float_as_uint(y[4 * r4 + 3])};
             __builtin_amdgcn_raw_buffer_store_b128(
-                w, obuf, offset_if(col0 + c < p.dv, row_at + 4 * c), 0, 0);
+                w, obuf, col0 + c < p.dv ? row_at + 4 * c : kNowhere, 0, 0);
           }
         }
       }
