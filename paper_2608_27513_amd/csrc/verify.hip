@@ -12,8 +12,11 @@
 // waits) runs over the sums to the piece that the drawn threshold falls into
 // and scans that one again. The largest rows are read once by many workgroups
 // and the rest of the work is a few kilobytes, in one launch: 128 requests of
-// 151001 fp32 tokens take 28 us (110 MB, 3.9 TB/s), one of 32000 6.9 us, which
-// is the launch and two chains of dependent loads.
+// 151001 fp32 tokens take 29 us (110 MB, 3.8 TB/s), one of 32000 6.3 us, which
+// is the launch and two chains of dependent loads. Twice the pieces in flight, by
+// a second set of registers, is slower (35 us: fewer waves).
+#include <algorithm>
+
 #include "device.hpp"
 #include "internal.hpp"
 
@@ -23,6 +26,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxDrafts = 1024;
+constexpr int kTickets = 65536;
 constexpr int kAhead = 4;  // pieces of a wave in flight
 
 struct VerifyParams {
@@ -33,11 +37,12 @@ struct VerifyParams {
   const float* u;
   int32_t* accepted;
   int32_t* out;
-  uint32_t* tickets;  // [65536], zero between calls
+  uint32_t* tickets;  // [65536], zero between calls; a request's is at b * spacing
   uint64_t* sums;     // [B, pieces]
   int32_t K, V;
   int32_t pieces;  // of a row
   int32_t steps;   // pieces of a wave
+  int32_t spacing;
 };
 
 template <typename T>
@@ -233,14 +238,16 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) 
   // The sums go through agent-scope atomic stores and loads, which pass the
   // L2 of their XCD, so they are in order with the ticket as soon as the stores
   // are acknowledged. A release fence would do, but writes back the whole L2
-  // for each workgroup (270 us against 28 at 128 requests of 151001 tokens).
+  // for each workgroup (270 us against 29 at 128 requests of 151001 tokens).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (t == 0) {
     const uint32_t ticket =
-        __hip_atomic_fetch_add(&v.tickets[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_fetch_add(&v.tickets[b * v.spacing], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     last = ticket == gridDim.x - 1;
-    if (last) __hip_atomic_store(&v.tickets[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (last)
+      __hip_atomic_store(&v.tickets[b * v.spacing], 0u, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if (!last) return;
@@ -290,10 +297,15 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) 
         i < a ? v.tokens[static_cast<size_t>(b) * v.K + i] : (i == a ? next : -1);
 }
 
-// Pieces of a wave: as few as let every workgroup be on the device at once (8
-// of 256 threads on each of 256 CUs), since each first follows the chain of
-// dependent loads to its row.
-constexpr int kWorkgroups = 2048;
+// Pieces of a wave: as few as make kWorkgroups workgroups, four on each of 256
+// CUs. Each first follows the chain of dependent loads to its row and ends with
+// an atomic, so more of them cost more than the loads that they add (64
+// requests of 131072 bf16 tokens: 512 / 1024 / 1536 / 2048 take 15.5 / 16.0 /
+// 17.6 / 17.5 us, 128 of 151001 fp32 tokens 34.9 / 30.3 / 30.1 / 30.2).
+constexpr int kWorkgroups = 1024;
+// Tickets of different requests in lines of their own, as far as there is room
+// (16 requests of 128000 tokens: 9.8 us against 30 side by side).
+constexpr int kTicketLine = 32;
 
 template <typename T>
 void launch(VerifyParams v, int B, hipStream_t s) {
@@ -302,11 +314,12 @@ void launch(VerifyParams v, int B, hipStream_t s) {
   const int64_t steps = (waves + kWorkgroups * kWaves - 1) / (kWorkgroups * kWaves);
   v.steps = static_cast<int32_t>(steps < v.pieces ? steps : v.pieces);
   const int blocks = (v.pieces + kWaves * v.steps - 1) / (kWaves * v.steps);
+  v.spacing = std::min(kTickets / B, kTicketLine);
   hipLaunchKernelGGL(verify_kernel<T>, dim3(blocks, B), dim3(kThreads), 0, s, v);
 }
 
 // Tickets have one place whatever B is: a workspace may serve any batch.
-constexpr size_t kTicketBytes = 65536 * sizeof(uint32_t);
+constexpr size_t kTicketBytes = kTickets * sizeof(uint32_t);
 
 }  // namespace
 }  // namespace damp

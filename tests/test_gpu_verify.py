@@ -47,10 +47,23 @@ def test_vocabularies(V, dtype):
         assert 0 < sum(got) < 45  # some drafts stand and some do not
 
 
-@pytest.mark.parametrize("B,K", [(1, 1), (1, 8), (3, 0), (64, 5), (300, 2), (2, 300)])
+@pytest.mark.parametrize("B,K", [(1, 1), (1, 8), (3, 0), (64, 5), (300, 2), (2, 300), (3001, 1)])
 def test_batches(B, K):
     print(f"verify B={B} K={K}", flush=True)
     check(*case(B + K, B, K, 997, noise=0.05))
+
+
+def test_the_largest_batch():
+    """65535 requests: more than have a line of their own for what counts their
+    workgroups, several of them each."""
+    print("verify B=65535", flush=True)
+    B, V = 65535, 300
+    p = torch.zeros(B, 1, V, device="cuda")
+    at = torch.arange(B, device="cuda") * 7 % V
+    p[torch.arange(B, device="cuda"), 0, at] = 0.5
+    a, o = S.damp_verify_drafts(p, p[:, :0], torch.zeros(B, 0, dtype=torch.int32, device="cuda"),
+                                torch.full((B, 1), 0.3, device="cuda"))
+    assert torch.equal(o[:, 0].long(), at) and not bool(a.any())
 
 
 def test_lengths():
