@@ -31,9 +31,10 @@
 // q, k, v and o set the floor: memory, as 4 d_k d_v operations a token and head
 // are few beside their bytes. What bounds the kernel is the issue of vector and matrix
 // instructions and the waits between them: at 32768 tokens, 32 heads of 128 and
-// o in bf16, three launches of 125 + 12 + 234 us, 185 TFLOP/s of the recurrence's
+// o in bf16, 376 us in three launches (128 + 12 + 237 at their fastest in a
+// profile, 137 + 12 + 252 at the median there), 183 TFLOP/s of the recurrence's
 // operations and 2.2 TB/s of the floor's bytes, the third launch with its matrix
-// units busy 37% and its vector issue 41% of the time, two waves a SIMD. Tried
+// units busy 36% and its vector issue 40% of the time, two waves a SIMD. Tried
 // and not kept: the parts of the next step placed between the products of this
 // one (the same time), a fourth wave that repeats a score tile to avoid the
 // branch (slower).

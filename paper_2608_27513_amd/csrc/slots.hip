@@ -5,7 +5,7 @@
 // multiple of 128) in each layer, and are bound by memory: a source is read
 // once and written once for each of its copies, 16 bytes a lane, past the
 // caches on both sides (what is copied is used much later, if at all): 8 slots
-// of 14.8 MB into 4 each take 99 us, 6.0 TB/s (117 us through the caches and
+// of 14.8 MB into 4 each take 98 us, 5.9 TB/s (117 us through the caches and
 // four words a lane, 111 with the words, 106 with two).
 //
 // The counts are kept by one workgroup each: pools have tens to thousands of

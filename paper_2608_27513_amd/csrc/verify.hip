@@ -12,9 +12,9 @@
 // waits) runs over the sums to the piece that the drawn threshold falls into
 // and scans that one again. The largest rows are read once by many workgroups
 // and the rest of the work is a few kilobytes, in one launch: 128 requests of
-// 151001 fp32 tokens take 29 us (110 MB, 3.8 TB/s), one of 32000 6.3 us, which
+// 151001 fp32 tokens take 30 us (110 MB, 3.7 TB/s), one of 32000 6.6 us, which
 // is the launch and two chains of dependent loads. Twice the pieces in flight, by
-// a second set of registers, is slower (35 us: fewer waves).
+// a second set of registers, is slower (36.6 us against 30.7, side by side).
 #include <algorithm>
 
 #include "device.hpp"
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) 
   // The sums go through agent-scope atomic stores and loads, which pass the
   // L2 of their XCD, so they are in order with the ticket as soon as the stores
   // are acknowledged. A release fence would do, but writes back the whole L2
-  // for each workgroup (270 us against 29 at 128 requests of 151001 tokens).
+  // for each workgroup (270 us against 30 at 128 requests of 151001 tokens).
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (t == 0) {
