@@ -83,6 +83,12 @@ __device__ __forceinline__ void fix40(float y, int& hi, int& lo) {
   lo = static_cast<int>((up - whole) * 1048576.0f);
 }
 
+// A uniform number cut to [0, 1 - 2^-24], NaN to 0. (fmaxf gives its other
+// operand for a NaN.)
+__device__ __forceinline__ float uniform(float u) {
+  return fminf(fmaxf(u, 0.0f), 1.0f - 0x1p-24f);
+}
+
 // The weight of a token as hi 2^20 + lo (lo may be negative).
 __device__ __forceinline__ void weight(float p, float q, int& hi, int& lo) {
   int hp, lp, hq, lq;
@@ -220,7 +226,8 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) 
       const float px = widen(static_cast<const T*>(v.p)[(row + b) * v.V + x]);
       const float qx = widen(static_cast<const T*>(v.q)[row * v.V + x]);
       // the product of two fp32 numbers is exact in double
-      stands = static_cast<double>(v.u[row + b]) * static_cast<double>(qx) < static_cast<double>(px);
+      stands = static_cast<double>(uniform(v.u[row + b])) * static_cast<double>(qx) <
+               static_cast<double>(px);
     }
     if (!stands) atomicMin(&first, i);
   }
@@ -270,9 +277,8 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyParams v) 
     if (i < wave) before += wave_total[i];
     total += wave_total[i];
   }
-  const float u = v.u[static_cast<size_t>(b) * (v.K + 1) + v.K];
-  const uint32_t r =
-      u > 0.0f ? min(static_cast<uint32_t>(fminf(u, 1.0f) * 16777216.0f), 0xffffffu) : 0u;
+  const uint32_t r = static_cast<uint32_t>(
+      uniform(v.u[static_cast<size_t>(b) * (v.K + 1) + v.K]) * 16777216.0f);
   const uint64_t threshold = (total >> 24) * r + (((total & 0xffffffu) * r) >> 24);
   if (threshold >= before && threshold < before + s) {
     uint64_t left = threshold - before;

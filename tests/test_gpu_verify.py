@@ -95,6 +95,38 @@ def test_drawn_numbers_at_their_ends():
     assert o[0, 0] == 4 and o[4, 0] == 4 and o[5, 0] == 4
 
 
+def cut(u):
+    """Uniform numbers as the definition takes them: in [0, 1 - 2^-24], NaN as 0."""
+    return u.nan_to_num(0.0, posinf=1.0, neginf=0.0).clamp(0.0, 1.0 - 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_judging_numbers_at_their_ends(dtype):
+    """The numbers that judge drafts are cut like the one that draws: 1 and more
+    accept a draft that is as probable as its target, none accepts one that the
+    target never makes, NaN and negative ones count as 0."""
+    print(f"verify judging ends {dtype}", flush=True)
+    ends = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, float("inf"), -1.0, float("-inf"),
+                         float("nan")])
+    B, V = len(ends), 600
+    p, q, tokens, u = case(15, B, 2, V, dtype)
+    rows = torch.arange(B)
+    equal, never = q.clone(), p.clone()
+    equal[:, 0] = p[:, 0]
+    never[rows, 0, tokens[:, 0].long()] = 0.0
+    u[:, 0] = ends
+    for target, draft, first in ((p, equal, True), (never, q, False)):
+        for other in (u[:, 1].clone(), ends.flip(0)):
+            now = u.clone()
+            now[:, 1] = other
+            host = lambda t: t.double().numpy()  # noqa: E731
+            want_a, want_o = ref.verify(host(target), host(draft), tokens.numpy(), host(cut(now)),
+                                        np.full(B, 2))
+            a, o = S.damp_verify_drafts(target.cuda(), draft.cuda(), tokens.cuda(), now.cuda())
+            assert a.tolist() == want_a.tolist() and o.tolist() == want_o.tolist()
+            assert ((a > 0) == first).all() and bool((o[rows, a.long()] >= 0).all())
+
+
 def test_one_token_has_all_the_weight():
     print("verify one", flush=True)
     for V, x in ((1, 0), (4096, 4095), (4097, 4096), (12345, 8191), (12345, 8192), (12345, 0)):
