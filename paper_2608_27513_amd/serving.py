@@ -5,6 +5,10 @@ and the slots of a state pool as the pages of its cache.
 Argument marshalling only, as in damp.py. Strides are the exception to its
 contiguous operands: q, k and v may keep any distance between tokens (a slice
 of a fused projection's output), and g may be one decay a head ([HV]).
+
+What a call allocates by itself, outputs and scratch, is allocated (and cleared)
+on the stream that it runs on, so that the memory is taken and given back in
+that stream's order.
 """
 from __future__ import annotations
 
@@ -57,6 +61,14 @@ def lib() -> ctypes.CDLL:
     return L
 
 
+def _new(make, shape, dtype, device, stream):
+    """make(shape) - torch.empty or torch.zeros - in the order of the call's stream."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
 def _ids(t, name: str, n=None) -> int:
     """The address of int32 device ids, [n] if n is given."""
     return _at(t, torch.int32, name, t.shape if n is None else (n,))
@@ -79,14 +91,14 @@ def _tokens(t, name: str, rows: int, heads: int, d: int):
     return t.data_ptr(), s[0] if rows > 1 else heads * d
 
 
-def _operands(pool: Pool, q, k, v, g, scale, o):
+def _operands(pool: Pool, q, k, v, g, scale, o, stream):
     """The arguments num_k_heads .. o_dtype of both linear-attention calls, and o."""
     HV, dk, dv = pool.num_v_heads, pool.layout.d_k, pool.layout.d_v
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a [tokens, HK, d_k] tensor")
     n, HK = q.shape[0], q.shape[1]
     if o is None:
-        o = torch.empty((n, HV, dv), dtype=torch.float32, device=q.device)
+        o = _new(torch.empty, (n, HV, dv), torch.float32, q.device, stream)
     if o.dtype is torch.float32:
         o_dt = D.DAMP_DT_FP32
     elif o.dtype is torch.bfloat16:
@@ -109,7 +121,7 @@ def damp_linear_update(pool: Pool, layer: int, slot_in, q, k, v, g, slot_out=Non
     """One token for each request (q, k [B, HK, d_k], v [B, HV, d_v], fp32 g
     [B, HV] or [HV]) from slot_in into slot_out (default: in place); returns
     o [B, HV, d_v]."""
-    args, o = _operands(pool, q, k, v, g, scale, o)
+    args, o = _operands(pool, q, k, v, g, scale, o, stream)
     B = q.shape[0]
     into = None if slot_out is None else _ids(slot_out, "slot_out", B)
     _check(lib().damp_linear_update(ctypes.byref(pool.desc), layer, _ids(slot_in, "slot_in", B),
@@ -128,13 +140,13 @@ def damp_linear_prefill(pool: Pool, layer: int, slot_in, q, k, v, g, seq_start, 
     int32 seq_start and seq_len [B]); returns o [tokens, HV, d_v], of which
     only the requests' tokens are written. Without a workspace one is
     allocated for the call."""
-    args, o = _operands(pool, q, k, v, g, scale, o)
+    args, o = _operands(pool, q, k, v, g, scale, o, stream)
     _ids(slot_in, "slot_in")
     B = slot_in.numel()
     into = None if slot_out is None else _ids(slot_out, "slot_out", B)
     if workspace is None:
-        workspace = torch.empty(damp_linear_prefill_workspace_bytes(pool, B, max_len),
-                                dtype=torch.uint8, device=q.device)
+        workspace = _new(torch.empty, damp_linear_prefill_workspace_bytes(pool, B, max_len),
+                         torch.uint8, q.device, stream)
     ws = _at(workspace, torch.uint8, "workspace", workspace.shape)
     _check(lib().damp_linear_prefill(ctypes.byref(pool.desc), layer, slot_in.data_ptr(), into, B,
                                      q.shape[0], max_len, _ids(seq_start, "seq_start", B),
@@ -166,12 +178,12 @@ def damp_verify_drafts(p, q, tokens, u, lens=None, workspace=None, accepted=None
         raise ValueError("p must be float32 or bfloat16")
     B, K, V = p.shape[0], p.shape[1] - 1, p.shape[2]
     if accepted is None:
-        accepted = torch.empty(B, dtype=torch.int32, device=p.device)
+        accepted = _new(torch.empty, B, torch.int32, p.device, stream)
     if out is None:
-        out = torch.empty((B, K + 1), dtype=torch.int32, device=p.device)
+        out = _new(torch.empty, (B, K + 1), torch.int32, p.device, stream)
     if workspace is None:
-        workspace = torch.zeros(damp_verify_workspace_bytes(B, V), dtype=torch.uint8,
-                                device=p.device)
+        workspace = _new(torch.zeros, damp_verify_workspace_bytes(B, V), torch.uint8, p.device,
+                         stream)
     ws = _at(workspace, torch.uint8, "workspace", workspace.shape)
     _check(lib().damp_verify_drafts(
         _at(p, p.dtype, "p", (B, K + 1, V)), _at(q, p.dtype, "q", (B, K, V)) if K else None, dtype,
@@ -187,7 +199,7 @@ def damp_verify_drafts(p, q, tokens, u, lens=None, workspace=None, accepted=None
 def damp_slots_alloc(refs, n: int, out=None, stream=None):
     """The n lowest free slots (int32 [n], -1 where none is left), each taken."""
     if out is None:
-        out = torch.empty(n, dtype=torch.int32, device=refs.device)
+        out = _new(torch.empty, n, torch.int32, refs.device, stream)
     _check(lib().damp_slots_alloc(_ids(refs, "refs"), refs.numel(), _ids(out, "out", n), n,
                                   _raw_stream(stream)))
     return out
@@ -224,12 +236,12 @@ def damp_slots_compact(pool: Pool, refs, workspace=None, map_out=None, live=None
     n = pool.num_slots
     dev = refs.device
     if map_out is None:
-        map_out = torch.empty(n, dtype=torch.int32, device=dev)
+        map_out = _new(torch.empty, n, torch.int32, dev, stream)
     if live is None:
-        live = torch.empty((), dtype=torch.int32, device=dev)
+        live = _new(torch.empty, (), torch.int32, dev, stream)
     if workspace is None:
-        workspace = torch.empty(damp_slots_compact_workspace_bytes(pool), dtype=torch.uint8,
-                                device=dev)
+        workspace = _new(torch.empty, damp_slots_compact_workspace_bytes(pool), torch.uint8, dev,
+                         stream)
     if live.numel() != 1:
         raise ValueError("live must hold one number")
     _check(lib().damp_slots_compact(ctypes.byref(pool.desc), _ids(refs, "refs", n),

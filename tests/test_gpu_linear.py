@@ -398,6 +398,46 @@ def test_streams_and_graphs():
         torch.randn(1000, device="cuda").sum().item()
 
 
+def test_a_stream_of_the_callers_with_the_bindings_scratch():
+    """Calls on a stream that is not torch's current one, outputs and scratch
+    allocated by the binding, while the current stream takes and frees memory:
+    the same results as on the current stream."""
+    print("own stream", flush=True)
+    lens = [700, 1, 64]
+    x = Setup(36, sum(lens), 4, 2, 64, 64, 3)
+    g, starts = x.g.cuda(), i32(np.concatenate([[0], np.cumsum(lens)[:-1]]))
+    ids, ls = i32([0, 1, 2]), i32(lens)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    p = torch.softmax(torch.randn(8, 4, 9000, generator=gen, device="cuda"), -1)
+    q = torch.softmax(torch.randn(8, 3, 9000, generator=gen, device="cuda"), -1)
+    drafts = torch.randint(0, 9000, (8, 3), generator=gen, device="cuda", dtype=torch.int32)
+    u = torch.rand(8, 4, generator=gen, device="cuda")
+    refs, first = i32([0, 1, 2]), x.now.clone()
+
+    def turn(stream=None):
+        r, kw = refs.clone(), dict(stream=stream)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        o = S.damp_linear_prefill(x.pool, 0, ids, *x.dev, g, starts, ls, 700, **kw)
+        o1 = S.damp_linear_update(x.pool, 0, ids, *(t[:3] for t in x.dev), g[:3], **kw)
+        a, out = S.damp_verify_drafts(p, q, drafts, u, **kw)
+        where, live = S.damp_slots_compact(x.pool, r, **kw)
+        if stream is not None:
+            for _ in range(8):  # what the calls above gave back is not the current stream's to take
+                torch.full((1 << 20,), -1, dtype=torch.int32, device="cuda")
+            stream.synchronize()
+        torch.cuda.synchronize()
+        return o, o1, a, out, where, live, r, x.now.clone()
+
+    want = turn()
+    assert S.damp_linear_prefill_workspace_bytes(x.pool, 3, 700) > 0
+    side = torch.cuda.Stream()
+    for i in range(3):
+        x.now.copy_(first)
+        got = turn(side)
+        assert all(torch.equal(s, t) for s, t in zip(got, want)), i
+
+
 def test_binding_refusals():
     x = Setup(34, 4, 4, 2, 64, 64, 4)
     g, ids = x.g.cuda(), i32([0, 1, 2, 3])

@@ -1,8 +1,10 @@
 """Host-side checks of the serving operators: exports, workspace sizes and
 refusals. No GPU needed: every call fails validation or has nothing to do."""
+import contextlib
 import ctypes
 import os
 import re
+import types
 
 import numpy as np
 import pytest
@@ -140,6 +142,64 @@ def test_slots_refusals(L):
         a = list(comp)
         a[i] = val
         assert L.damp_slots_compact(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+
+
+# ------------------------------------------------ what the binding allocates
+
+class FakeStream:
+    cuda_stream = 0x1234
+
+
+@pytest.mark.parametrize("stream", [None, FakeStream()])
+def test_allocations_are_made_on_the_calls_stream(L, monkeypatch, stream):
+    """Outputs and scratch that the binding allocates, and the zeros that the
+    verification's has to start with, are made while the call's stream is
+    torch's current one."""
+    current, made, launched = [None], [], []
+
+    @contextlib.contextmanager
+    def on(s):
+        before, current[0] = current[0], s
+        yield
+        current[0] = before
+
+    def recorded(make):
+        def run(shape, **kw):
+            made.append(current[0])
+            return make(shape, dtype=kw["dtype"])
+        return run
+
+    class Calls:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return lambda *a: 64
+            return lambda *a: launched.append((name, a[-1])) or 0
+
+    empty, zeros, i32 = torch.empty, torch.zeros, torch.int32
+    layout = D.damp_layout_init(64, 64, 0, D.DAMP_STATE_FP32)
+    pool = types.SimpleNamespace(num_v_heads=2, num_slots=4, layout=layout, desc=D.damp_pool())
+    q = zeros(4, 2, 64, dtype=torch.bfloat16)
+    g, ids, refs = zeros(4, 2), zeros(4, dtype=i32), zeros(4, dtype=i32)
+    p, u = zeros(4, 2, 8), zeros(4, 2)
+    drafts, names = zeros(4, 1, 8), zeros(4, 1, dtype=i32)
+    monkeypatch.setattr(S, "lib", Calls)
+    monkeypatch.setattr(S, "_at", lambda t, *a: t.data_ptr())
+    monkeypatch.setattr(S, "_tokens", lambda t, name, n, h, d: (t.data_ptr(), h * d))
+    monkeypatch.setattr(S, "_raw_stream", lambda s=None: 0 if s is None else s.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", recorded(empty))
+    monkeypatch.setattr(torch, "zeros", recorded(zeros))
+    for call, allocations in (
+            (lambda **kw: S.damp_linear_update(pool, 0, ids, q, q, q, g, **kw), 1),
+            (lambda **kw: S.damp_linear_prefill(pool, 0, ids, q, q, q, g, ids, ids, 1, **kw), 2),
+            (lambda **kw: S.damp_verify_drafts(p, drafts, names, u, **kw), 3),
+            (lambda **kw: S.damp_slots_alloc(refs, 3, **kw), 1),
+            (lambda **kw: S.damp_slots_compact(pool, refs, **kw), 3)):
+        made.clear()
+        launched.clear()
+        call(stream=stream)
+        assert made == [stream] * allocations
+        assert [s for _, s in launched] == [0 if stream is None else stream.cuda_stream]
 
 
 # ----------------------------------------- the plain implementations themselves
