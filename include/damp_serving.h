@@ -38,7 +38,9 @@ extern "C" {
  *   S_t = exp(g_t) S_{t-1} + k_t v_t^T
  *   o_t = scale * S_t^T q_t            (from the updated state)
  * with g_t one fp32 number per token and head (a log-decay; 0 keeps the
- * state, -inf forgets it). The states live in a DAMP_STATE_FP32 pool with
+ * state, -inf forgets it, up to 88, whose factor fp32 just holds, grows it).
+ * Over any number of tokens that grow, results are the recurrence's as long as
+ * its own states and outputs stay in fp32. The states live in a DAMP_STATE_FP32 pool with
  * d_k and d_v multiples of 8 up to 256, not necessarily equal. Other pools
  * return DAMP_ERR_UNSUPPORTED.
  *

@@ -26,7 +26,11 @@
 //
 // Log-decays are summed in double, in units of log2: their differences stay
 // good to fp32 however far the sum has run. A log-decay below -1000 counts as
-// that (its factor is 0 in fp32 either way), so -inf makes no inf - inf.
+// that (its factor is 0 in fp32 either way), so -inf makes no inf - inf. Where
+// log-decays are positive a chunk ends before their sum passes kMostGrowth (one
+// token alone may): a factor over more tokens would lose digits, and leave fp32
+// where what it multiplies is 0 or tiny. The factor of a segment has an exponent
+// of its own for the same reason.
 //
 // q, k, v and o set the floor: memory, as 4 d_k d_v operations a token and head
 // are few beside their bytes. What bounds the kernel is the issue of vector and matrix
@@ -62,13 +66,14 @@ constexpr int kBufferConfig = 0x00020000;  // raw 32-bit buffer (gfx9 family)
 constexpr uint32_t kNowhere = 0x80000000u;  // past the end of every buffer here
 constexpr float kLeastLog = -1000.0f;
 constexpr double kLog2e = 1.4426950408889634;
+constexpr double kMostGrowth = 16.0;  // log2; exponents below it are good to 2^-21 in fp32
 
 struct PromptParams {
   LinearParams l;
   const int32_t* seq_start;
   const int32_t* seq_len;
   float* seg_states;  // [B, segments, HV, dk, dv]
-  float* seg_decays;  // [B, segments, HV]
+  float2* seg_decays;  // [B, segments, HV]: x 2^y, 1 <= x <= 2
   int32_t n_tokens;
   int32_t max_len;
   int32_t seg_len;   // tokens, a multiple of kChunk
@@ -174,6 +179,24 @@ __device__ __forceinline__ double wave_scan_f64(double x) {
   return x;
 }
 
+// 2^x with fp32's digits however large |x| is.
+__device__ __forceinline__ float exp2_f32(double x) {
+  const double whole = floor(x);
+  return ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(whole));
+}
+
+// 2^x in double, by the series of e^y to y^9 at |y| <= ln(2) / 2 (7e-12 of it is
+// left out). A loop: its constants would be kept in registers otherwise.
+__constant__ const double kInverseFactorial[10] = {
+    1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880};
+__device__ __forceinline__ double exp2_f64(double x) {
+  const double whole = __builtin_rint(x), y = (x - whole) * 0.6931471805599453;
+  double sum = 0.0;
+#pragma clang loop unroll(disable)
+  for (int n = 9; n >= 0; --n) sum = fma(sum, y, kInverseFactorial[n]);
+  return ldexp(sum, static_cast<int>(whole));
+}
+
 // PARTS = 0: the first pass, which leaves the state of each segment but the
 // last from a zero start. PARTS = 2 or 3: outputs, with so many parts of S
 // and P.
@@ -199,6 +222,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
   __shared__ __attribute__((aligned(16))) float to_end[2][kChunk];
   __shared__ float from_start[2][kChunk];  // times the scale
   __shared__ float chunk_decay[2];
+  __shared__ int chunk_len[2];
 
   // Branches from here on go by scalars. In a branch that only some lanes or
   // waves take, the compiler may save a register before the others are back,
@@ -321,15 +345,38 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     gr = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
         gbuf, offset_if(lane < rows, lane * static_cast<uint32_t>(g_row)), 0, 0));
   };
+  // Returns the chunk's tokens, of those that its rows hold.
+  float owed = 0.0f;  // what growing chunks' factors were rounded by, relative
   auto scan_g = [&](int to_buf) {
     const double s = wave_scan_f64(static_cast<double>(gr < kLeastLog ? kLeastLog : gr) * kLog2e);
-    const double all = __shfl(s, 63, 64);
+    double all = __shfl(s, 63, 64);
+    int n = kChunk;
+    float left = exp2_f32(all - s), whole = exp2_f32(all);
+    // (once a chunk's factor has been rounded so, all later ones make up for it)
+    if (__builtin_amdgcn_ballot_w64(gr > 0.0f || owed != 0.0f) != 0) {
+      const double growth = wave_scan_f64(static_cast<double>(gr > 0.0f ? gr : 0.0f) * kLog2e);
+      const uint64_t past = __builtin_amdgcn_ballot_w64(!(growth <= kMostGrowth));
+      if (past != 0) {
+        n = max(static_cast<int>(__builtin_ctzll(past)), 1);
+        all = __shfl(s, n - 1, 64);
+        // the rows past the chunk's tokens add nothing to the state
+        left = lane < n ? exp2_f32(all - s) : 0.0f;
+      }
+      // what grows carries the rounding of every factor since: each makes up
+      // for those before it
+      const double exact = exp2_f64(all) * (1.0 + owed);
+      whole = static_cast<float>(exact);
+      owed = static_cast<float>(exact - whole) * __builtin_amdgcn_rcpf(whole);
+      owed = fabsf(owed) < 0x1p-20f ? owed : 0.0f;  // of 0, of an infinity: nothing
+    }
     run_log += all;
     const double coarse = __builtin_rint(s * 64.0) * 0.015625;
     logs[to_buf][lane] = make_float2(static_cast<float>(coarse), static_cast<float>(s - coarse));
-    to_end[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(all - s));
-    from_start[to_buf][lane] = __builtin_amdgcn_exp2f(static_cast<float>(s)) * p.scale;
-    chunk_decay[to_buf] = __builtin_amdgcn_exp2f(static_cast<float>(all));
+    to_end[to_buf][lane] = left;
+    from_start[to_buf][lane] = exp2_f32(s) * p.scale;
+    chunk_decay[to_buf] = whole;
+    chunk_len[to_buf] = n;
+    return n;
   };
 
   auto stage = [&] {
@@ -344,31 +391,31 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       *reinterpret_cast<u32x4*>(vt + (t / (4 * NW) + vRows * i) * VS + 8 * v8) = vr[i];
   };
 
+  int n = kChunk;  // tokens of the chunk
   if (count > 0) {
     const Rows head = rows(0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(head, i);
     if (decays) {
       load_g(0);
-      scan_g(0);
-      load_g(kChunk);
+      load_g(scan_g(0));
     }
     stage();
+    __syncthreads();  // the first chunk is there
+    n = __builtin_amdgcn_readfirstlane(chunk_len[0]);
     // (past the end the buffers are empty and their loads give zeros)
-    const Rows next = rows(kChunk);
+    const Rows next = rows(n);
 #pragma unroll
     for (int i = 0; i < (kOut ? KV : kLoads); ++i) load(next, i);
   }
-  for (int first = 0; first < count; first += kChunk) {
-    const int buf = (first / kChunk) & 1;
-    const bool more = first + kChunk < count;
-    __syncthreads();  // the chunk is there
-
+  int buf = 0, next_n = kChunk;
+  for (int first = 0; first < count; first += n, n = next_n, buf ^= 1) {
+    const bool more = first + n < count;
     const float all = chunk_decay[buf];
     const bool whole = PARTS != 2 || (seg == segs - 1 && keep);
     f32x16 O[2];
     if constexpr (kOut) {
-      const Rows soon = rows(first + kChunk);
+      const Rows soon = rows(first + n);
       // ---- scores of tiles (tokens j, tokens i): (0, 0), (0, 1), (1, 1)
       for (int w = wave; w < 3; w += NW) {
         const int jt = w >> 1, it = (w + 1) >> 1;
@@ -479,13 +526,11 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     }
 
     // ---- the next decays; then P is there, and K, Q and V have been read
-    if (decays && more) {
-      scan_g(buf ^ 1);
-      load_g(first + 2 * kChunk);
-    }
+    if (decays && more) load_g(first + n + scan_g(buf ^ 1));
     __syncthreads();
     if (more) stage();
-    const Rows ahead = rows(first + 2 * kChunk);
+    next_n = more ? __builtin_amdgcn_readfirstlane(chunk_len[buf ^ 1]) : kChunk;
+    const Rows ahead = rows(first + n + next_n);
     if constexpr (!kOut) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) load(ahead, i);
@@ -503,7 +548,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       }
       const auto obuf = rows_of(static_cast<uint8_t*>(p.o) + (static_cast<int64_t>(h) * p.dv + col0) *
                                                                  (p.o_bf16 ? 2 : 4),
-                                tok0 + first, o_row, count - first);
+                                tok0 + first, o_row, min(count - first, n));
 #pragma unroll
       for (int it = 0; it < 2; ++it) {
         const uint32_t row_at = (32 * it + n32) * static_cast<uint32_t>(o_row);
@@ -537,6 +582,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
         }
       }
     }
+    __syncthreads();  // the next chunk is there
   }
 
   // ---- the state after the last token
@@ -546,9 +592,11 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
       dst = reinterpret_cast<float*>(p.layer_base + to * p.slot_stride + h * p.tile_stride);
   } else {
     dst = pp.seg_states + tile + seg * tile_step;
-    if (decays && col0 == 0)
-      pp.seg_decays[(static_cast<size_t>(b) * pp.segments + seg) * p.HV + h] =
-          __builtin_amdgcn_exp2f(static_cast<float>(run_log));
+    if (decays && col0 == 0) {
+      const double whole = floor(fmin(fmax(run_log, -4096.0), 4096.0));
+      pp.seg_decays[(static_cast<size_t>(b) * pp.segments + seg) * p.HV + h] = make_float2(
+          __builtin_amdgcn_exp2f(static_cast<float>(run_log - whole)), static_cast<float>(whole));
+    }
   }
   if (dst) {
     const auto sbuf = state_buffer(dst, p);
@@ -580,17 +628,18 @@ __global__ __launch_bounds__(256) void prompt_states(const PromptParams pp) {
   const size_t step = static_cast<size_t>(p.HV) * p.dk * p.dv;
   float* state = pp.seg_states + static_cast<size_t>(b) * pp.segments * step +
                  static_cast<size_t>(h) * p.dk * p.dv + at;
-  const float* decay = pp.seg_decays + static_cast<size_t>(b) * pp.segments * p.HV + h;
+  const float2* decay = pp.seg_decays + static_cast<size_t>(b) * pp.segments * p.HV + h;
   for (int s = 0; s < segs; ++s) {
     float4* place = reinterpret_cast<float4*>(state + s * step);
     const bool last = s == segs - 1;
     const float4 add = last ? x : *place;
-    const float d = last ? 0.0f : decay[static_cast<size_t>(s) * p.HV];
+    const float2 d = last ? make_float2(0.0f, 0.0f) : decay[static_cast<size_t>(s) * p.HV];
+    const int e = static_cast<int>(d.y);
     *place = x;
-    x.x = fmaf(d, x.x, add.x);
-    x.y = fmaf(d, x.y, add.y);
-    x.z = fmaf(d, x.z, add.z);
-    x.w = fmaf(d, x.w, add.w);
+    x.x = fmaf(d.x, ldexpf(x.x, e), add.x);
+    x.y = fmaf(d.x, ldexpf(x.y, e), add.y);
+    x.z = fmaf(d.x, ldexpf(x.z, e), add.z);
+    x.w = fmaf(d.x, ldexpf(x.w, e), add.w);
   }
 }
 
@@ -627,7 +676,7 @@ Split split_of(const damp_pool* pool, int32_t B, int64_t n_tokens, int32_t max_l
 size_t workspace_bytes_of(const damp_pool* pool, int32_t B, const Split& s) {
   if (s.segments < 2) return 0;
   const size_t tiles = static_cast<size_t>(B) * s.segments * pool->num_v_heads;
-  return tiles * (static_cast<size_t>(pool->layout.d_k) * pool->layout.d_v + 1) * sizeof(float);
+  return tiles * (static_cast<size_t>(pool->layout.d_k) * pool->layout.d_v * sizeof(float) + sizeof(float2));
 }
 
 template <int DK, int NW>
@@ -708,7 +757,8 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
   p.seg_len = split.seg_len;
   p.segments = split.segments;
   p.seg_states = static_cast<float*>(workspace);
-  p.seg_decays = p.seg_states + static_cast<size_t>(B) * split.segments * p.l.HV * p.l.dk * p.l.dv;
+  p.seg_decays = reinterpret_cast<float2*>(
+      p.seg_states + static_cast<size_t>(B) * split.segments * p.l.HV * p.l.dk * p.l.dv);
   if (p.l.dk <= 64) launch<64>(p, B, s);
   else if (p.l.dk <= 128) launch<128>(p, B, s);
   else launch<256>(p, B, s);

@@ -154,8 +154,9 @@ def test_update_decays():
 # ------------------------------------------------------------------ prompts
 
 def run_prompts(x, lens, slot_in, slot_out, *, o_type=torch.float32, starts=None, max_len=None,
-                workspace=None, poison=False):
-    """Runs packed prompts and checks outputs and every state of the pool."""
+                workspace=None, poison=False, check=check_o):
+    """Runs packed prompts and checks outputs (by `check`) and every state of
+    the pool."""
     slots = x.state.shape[0]
     starts = np.concatenate([[0], np.cumsum(lens)[:-1]]) if starts is None else starts
     o = torch.full((x.n, x.HV, x.dv), 7.0, dtype=o_type, device="cuda")
@@ -175,7 +176,7 @@ def run_prompts(x, lens, slot_in, slot_out, *, o_type=torch.float32, starts=None
         into = (slot_in if slot_out is None else slot_out)[b]
         if 0 <= into < slots:
             state[into] = S1.float()
-    check_o(o[covered], want[covered], lens)
+    check(o[covered], want[covered], lens)
     assert bool((o[~covered.cuda()] == 7.0).all())
     assert rel(x.now, state) <= FP32, lens
     return o
@@ -288,6 +289,89 @@ def test_prompt_decays():
     run_prompts(x, [T], [1], [0])
     x = Setup(26, 2 * T, 6, 3, 128, 64, 2, decay=lambda g: torch.cat([decay(g[:T]), decay(g[T:])]))
     run_prompts(x, [T + 3, T - 3], [0, -1], [0, 1])
+
+
+def check_terms(x, o, start, length, slot):
+    """bf16 outputs of one request: half a step of bf16, and of the sum of the
+    terms' absolute values 2^-18 for the state's and 2^-18 for the scores' two
+    bf16 parts (each leaves 2^-9 of what it is rounded from), and fp32's."""
+    q, k, v = (t[start:start + length].abs() for t in x.cpu)
+    S0 = x.state[slot].abs() if slot >= 0 else torch.zeros_like(x.state[0])
+    terms, _ = ref.linear(q, k, v, x.g[start:start + length], S0, x.scale)
+    want, _ = x.want(start, length, slot)
+    got = o[start:start + length].double().cpu()
+    assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -17 + FP32) * terms).all())
+
+
+GROWTH = {  # log-decays [T] and whether values are 0 while they grow
+    # a new request whose first values are 0: its state stays 0 whatever grows
+    "zeros": (lambda t: torch.where(t < 150, 3.0, -0.1), True),
+    # a state of 1e-30 that grows by e^100
+    "tiny": (lambda t: torch.where(t < 150, 100 / 150, -0.1), True),
+    # steady growth, e^60 in all
+    "steady": (lambda t: torch.full(t.shape, 60 / len(t)), False),
+    # single tokens that grow by more than a chunk may, and back
+    "back and forth": (lambda t: torch.where(t % 2 == 0, 30.0, -30.0), False),
+    # one large factor a token, each forgotten by the next
+    "resets": (lambda t: torch.where(t % 3 == 1, 60.0, float("-inf")), False),
+    # growth in one token of many
+    "single": (lambda t: torch.where(t % 50 == 49, 20.0, -1.0), False),
+}
+
+
+@pytest.mark.parametrize("what", GROWTH)
+@pytest.mark.parametrize("T,dk,dv,HV", [(200, 64, 64, 2), (40, 128, 128, 2), (200, 128, 128, 4),
+                                        (700, 128, 48, 2), (300, 256, 72, 1)])
+@pytest.mark.parametrize("o_type", [torch.float32, torch.bfloat16])
+def test_prompt_growth(what, T, dk, dv, HV, o_type):
+    """Positive log-decays: the factor of many tokens may leave fp32 where the
+    recurrence, whose states are 0, tiny or forgotten, does not. bf16 outputs
+    are bounded by the sizes of their own terms: rows differ by many orders
+    here, and a state that one token dominates leaves rows in which all terms
+    cancel."""
+    print(f"prompt growth {what} {T} {dk}x{dv} {HV} {o_type}", flush=True)
+    g, quiet = GROWTH[what]
+    t = torch.arange(T)
+    # the first head grows, the others decay beside it
+    x = Setup(50, T, HV, 1, dk, dv, 2, decay=lambda d: torch.cat([g(t)[:, None], d[:, 1:]], 1))
+    if quiet:
+        x.cpu[2][:150, 0] = 0.0
+        x.dev[2] = x.cpu[2].contiguous().cuda()
+    if what == "tiny":
+        x.state[:, 0] *= 1e-30
+        x.now.copy_(x.state)
+    slot = -1 if what == "zeros" else 1
+    if o_type is torch.bfloat16:
+        o = run_prompts(x, [T], [slot], [0], o_type=o_type, check=lambda *_: None)
+        check_terms(x, o, 0, T, slot)
+        return
+    o = run_prompts(x, [T], [slot], [0])
+    w, S1 = x.want(0, T, slot)
+    for h in range(HV):  # each head on its own: growth makes them unlike
+        assert rel(o[:, h], w[:, h]) <= FP32 and rel(x.now[0, h], S1[h]) <= FP32, h
+
+
+def test_prompt_growth_beside_others():
+    """Requests of one call whose chunks end at different tokens."""
+    print("prompt growth beside", flush=True)
+    lens = [200, 64, 130, 1, 500]
+    n = sum(lens)
+
+    def decay(g):
+        g = g.clone()
+        g[50:150, 1] = 0.5
+        g[264:394:7, 0] = 25.0
+        g[264 + 3:394:7, 0] = -25.0
+        g[400:500] = 0.2
+        return g
+
+    x = Setup(51, n, 4, 2, 128, 128, 10, decay=decay)
+    run_prompts(x, lens, [0, 1, 2, 3, 4], [5, 6, 2, 8, 9])
+    x = Setup(51, n, 4, 2, 128, 128, 10, decay=decay)
+    o = run_prompts(x, lens, [0, 1, 2, 3, 4], [5, 6, 2, 8, -1], o_type=torch.bfloat16,
+                    check=lambda *_: None)
+    for b, at in enumerate([0, 200, 264, 394, 395]):
+        check_terms(x, o, at, lens[b], b)
 
 
 def test_prompt_resets_keep_precision():
