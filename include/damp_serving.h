@@ -167,7 +167,9 @@ damp_status damp_verify_drafts(const void* p, const void* q, int32_t dtype,
  * ---------------------------------------------------------------------- */
 
 /* Takes the n lowest free slots in ascending order: out[i] (int32 [n]) is
- * the slot and its count becomes 1; -1 where no slot is left. */
+ * the slot and its count becomes 1; -1 where no slot is left. (To the linear
+ * calls -1 is DAMP_SLOT_ZERO: a caller that does not know that n slots are free
+ * has to look before it passes the ids on.) */
 damp_status damp_slots_alloc(int32_t* refs, int32_t num_slots, int32_t* out,
                              int32_t n, void* stream);
 

@@ -84,13 +84,16 @@ def random_weights(seed: int, *, layers=4, HV=4, HK=2, d=64, vocab=1000, tempera
 
 class Server:
     """Requests of one target model and its draft, their slots, and rounds of
-    speculation over all of them."""
+    speculation over all of them. How many slots requests hold is known on the
+    host too: an id of no slot left (-1) is the zero state to the linear calls,
+    so requests that do not fit have to be refused before they are allocated."""
 
     def __init__(self, weights, *, draft_layers: int, slots: int, drafts: int, seed: int = 0,
                  device="cuda"):
         self.target = Model(weights, len(weights["layers"]), slots)
         self.draft = Model(weights, draft_layers, slots)
         self.K, self.dev = drafts, device
+        self.slots, self.held = slots, 0
         self.refs = torch.zeros(slots, dtype=torch.int32, device=device)
         self.gen = torch.Generator(device=device).manual_seed(seed)
         vocab = weights["embed"].shape[0]
@@ -110,7 +113,16 @@ class Server:
 
     def admit(self, prompts, samples: int):
         """Prefills the prompts (host lists) together and forks each into
-        `samples` requests; returns (slots, pending tokens) of all of them."""
+        `samples` requests; returns (slots, pending tokens) of all of them.
+        Raises ValueError where they, or the scratch slots that a round of
+        drafts takes for each request, would not fit."""
+        if samples < 1 or not all(prompts):
+            raise ValueError("needs at least one sample, and a token in every prompt")
+        held = self.held + len(prompts) * samples
+        if held * (2 if self.K else 1) > self.slots:
+            raise ValueError(f"{held} requests{' with a scratch slot each' if self.K else ''} "
+                             f"do not fit {self.slots} slots")
+        self.held = held
         lens = [len(x) - 1 for x in prompts]  # the last token is the first to be stepped
         starts = [sum(lens[:i]) for i in range(len(lens))]
         i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=self.dev)  # noqa: E731
@@ -128,7 +140,7 @@ class Server:
         """K drafts, their verification and the states moved on; returns
         (accepted [B], tokens [B, K + 1], pending)."""
         B, K = slots.numel(), self.K
-        scratch = S.damp_slots_alloc(self.refs, B)
+        scratch = S.damp_slots_alloc(self.refs, B if K else 0)
         tokens, dists = [pending], []
         for i in range(K):
             q = self.draft.step(tokens[-1], slots if i == 0 else scratch, scratch)
@@ -158,6 +170,7 @@ class Server:
         S.damp_slots_compact(self.draft.pool, again)
         keep = torch.ones(slots.numel(), dtype=torch.bool, device=self.dev)
         keep[ended] = False
+        self.held -= int((~keep).sum())
         return where[slots[keep].long()], keep
 
 

@@ -89,6 +89,37 @@ def test_states_after_rounds_are_those_of_the_text():
         assert float((a - b).norm() / b.norm()) <= 2.0 ** -8
 
 
+def test_requests_that_do_not_fit_are_refused():
+    """Nothing is allocated for them; what fits, with a scratch slot for each
+    request, runs, also after others have ended."""
+    print("speculate full", flush=True)
+    w = X.random_weights(8, vocab=200)
+    server = X.Server(w, draft_layers=2, slots=9, drafts=2)
+    ps = prompts([5, 9, 3], 200)
+    for bad in ((ps, 2), (ps[:1], 5), ([[]], 1), (ps, 0)):
+        with pytest.raises(ValueError):
+            server.admit(*bad)
+    assert server.refs.tolist() == [0] * 9
+    slots, pending = server.admit(ps[:2], 2)
+    assert (slots >= 0).all()
+    with pytest.raises(ValueError, match="9 slots"):
+        server.admit(ps[2:], 1)
+    assert int(server.refs.sum()) == 4
+    _, _, pending = server.round(slots, pending)
+    slots, keep = server.end(slots, torch.tensor([1, 2], device="cuda"))
+    more, again = server.admit(ps[2:], 2)
+    assert sorted(slots.tolist() + more.tolist()) == [0, 1, 2, 3]
+    server.round(torch.cat([slots, more]), torch.cat([pending[keep], again]))
+    assert int(server.refs.sum()) == 4
+    with pytest.raises(ValueError):
+        server.admit(ps[:1], 1)
+    whole = X.Server(w, draft_layers=1, slots=3, drafts=0)  # no drafts: no scratch
+    slots, pending = whole.admit(ps, 1)
+    whole.round(slots, pending)
+    with pytest.raises(ValueError, match="4 requests do not fit 3 slots"):
+        whole.admit(ps[:1], 1)
+
+
 def test_main_runs(capsys):
     X.main()
     assert "tokens" in capsys.readouterr().out
