@@ -19,6 +19,9 @@ from . import damp as D
 from . import serving as S
 
 
+PADDED = -2  # a slot id of no slot and not the zero state: a request that is not run
+
+
 class Model:
     """Layers of linear attention with residuals over a tied embedding, and the
     state pool of their requests."""
@@ -138,12 +141,17 @@ class Server:
 
     def round(self, slots, pending):
         """K drafts, their verification and the states moved on; returns
-        (accepted [B], tokens [B, K + 1], pending)."""
+        (accepted [B], tokens [B, K + 1], pending). A next token of -1 (no token
+        had weight) ends its request: from the next round on it takes part as a
+        padded one, with -1 accepted, tokens of -1 and its state left alone."""
         B, K = slots.numel(), self.K
+        live = pending >= 0
+        slots = torch.where(live, slots, PADDED)
         scratch = S.damp_slots_alloc(self.refs, B if K else 0)
+        from_scratch = torch.where(live, scratch, PADDED) if K else scratch
         tokens, dists = [pending], []
         for i in range(K):
-            q = self.draft.step(tokens[-1], slots if i == 0 else scratch, scratch)
+            q = self.draft.step(tokens[-1], slots if i == 0 else from_scratch, scratch)
             tokens.append(self.sample(q))
             dists.append(q)
         S.damp_slots_release(self.refs, scratch)
@@ -156,10 +164,12 @@ class Server:
         q = torch.stack(dists, 1) if K else p.new_empty(B, 0, p.shape[1])
         accepted, out = S.damp_verify_drafts(p.view(B, K + 1, -1), q, run[:, 1:].contiguous(),
                                              self.uniform(B, K + 1), workspace=self.ws)
+        accepted = torch.where(live, accepted, -1)
+        out = torch.where(live[:, None], out, -1)
         stands = accepted + 1
         self.target.replay(kept, slots, start, stands, K + 1)
         self.draft.prompt(flat, slots, slots, start, stands, K + 1)
-        return accepted, out, out.gather(1, accepted[:, None].long())[:, 0]
+        return accepted, out, out.gather(1, accepted[:, None].clamp(min=0).long())[:, 0]
 
     def end(self, slots, ended):
         """Releases the requests at the indices `ended`, compacts both pools and

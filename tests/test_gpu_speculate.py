@@ -120,6 +120,36 @@ def test_requests_that_do_not_fit_are_refused():
         whole.admit(ps[:1], 1)
 
 
+def test_a_request_without_a_next_token_ends():
+    """A next token of -1 is no token: its request stands still from then on,
+    the others go on."""
+    print("speculate end", flush=True)
+    w = X.random_weights(9, vocab=200)
+    server = X.Server(w, draft_layers=2, slots=8, drafts=3)
+    slots, pending = server.admit(prompts([5, 9, 3], 200), 1)
+
+    def states(slot):
+        return [m.pool.buffer.view(len(m.w["layers"]), 8, -1)[:, slot].clone()
+                for m in (server.target, server.draft)]
+
+    ended, live = int(slots[1]), int(slots[0])
+    pending[1] = -1
+    before, running = states(ended), states(live)
+    for _ in range(2):
+        accepted, out, pending = server.round(slots, pending)
+        assert accepted.tolist()[1] == -1 and out[1].tolist() == [-1] * 4 and int(pending[1]) == -1
+        assert (accepted[[0, 2]] >= 0).all() and (pending[[0, 2]] >= 0).all()
+    assert all(torch.equal(a, b) for a, b in zip(before, states(ended)))
+    assert not any(torch.equal(a, b) for a, b in zip(running, states(live)))
+    server.target.w["out"] = torch.full_like(w["out"], float("nan"))  # no token has weight
+    accepted, out, pending = server.round(slots, pending)
+    assert accepted.tolist() == [0, -1, 0] and pending.tolist() == [-1] * 3
+    before = states(live)
+    accepted, _, pending = server.round(slots, pending)
+    assert accepted.tolist() == [-1] * 3 and pending.tolist() == [-1] * 3
+    assert all(torch.equal(a, b) for a, b in zip(before, states(live)))
+
+
 def test_main_runs(capsys):
     X.main()
     assert "tokens" in capsys.readouterr().out
