@@ -37,7 +37,4 @@ damp_status linear_params(const char* name, const damp_pool* pool, int32_t layer
                           const float* g, int64_t g_stride, float scale, void* o, int32_t o_dtype,
                           hipStream_t stream, LinearParams* p);
 
-// Compute units of the current device (0 if it cannot be asked).
-int device_cus();
-
 }  // namespace damp

@@ -16,14 +16,6 @@
 
 namespace damp {
 
-int device_cus() {
-  int dev = 0, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
-    return 0;
-  return n;
-}
-
 namespace {
 
 // With DAMP_CHECK_SLOTS set: a slot that one request writes is written and
