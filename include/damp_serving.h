@@ -83,7 +83,8 @@ damp_status damp_linear_update(const damp_pool* pool, int32_t layer,
 
 /* Scratch of damp_linear_prefill for B requests of at most max_len tokens
  * (0 where it needs none, and for invalid arguments). Its contents matter
- * only during a call. */
+ * only during a call. More or longer requests may need less, since fewer
+ * pieces of them fill the device: ask for each call's B and max_len. */
 size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B,
                                            int32_t max_len);
 

@@ -647,8 +647,9 @@ __global__ __launch_bounds__(256) void prompt_states(const PromptParams pp) {
 // requests share n_tokens and none is longer than max_len. Segments are as
 // long as leave every CU its two workgroups, at least kLeastSegment tokens (a
 // request of up to kUncut is not cut: the two other launches would cost more),
-// and no shorter than the finest cut, which goes by B and max_len alone and
-// which the workspace has room for. Measured on 256 CUs, in us: one request of
+// and no shorter than the finest cut, which goes by B and max_len alone. More
+// tokens never make shorter segments, so the workspace for n_tokens = max_len,
+// the least there can be, has room for all of a B and max_len. Measured on 256 CUs, in us: one request of
 // 32768 tokens and 32 heads in 512 / 1024 / 2048 / 4096 pieces 391 / 416 / 444
 // / 522; eleven of 1 to 4096 tokens in 240 / 490 / 970: 214 / 155 / 157; one
 // of 200 whole 22, in two 27; one of 500 in segments of 128 / 256: 30 / 40.
@@ -711,7 +712,7 @@ extern "C" {
 size_t damp_linear_prefill_workspace_bytes(const damp_pool* pool, int32_t B, int32_t max_len) {
   using namespace damp;
   if (check_pool(pool) != DAMP_OK || B <= 0 || B > 65535 || max_len < 0) return 0;
-  return workspace_bytes_of(pool, B, split_of(pool, B, 0, max_len));
+  return workspace_bytes_of(pool, B, split_of(pool, B, max_len, max_len));
 }
 
 damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int32_t* slot_in,
@@ -745,7 +746,7 @@ damp_status damp_linear_prefill(const damp_pool* pool, int32_t layer, const int3
       static_cast<int64_t>(p.l.HV) * p.l.dv > kMost)
     return fail(DAMP_ERR_INVALID_ARG, "%s: a token's row is too long", name);
   const Split split = split_of(pool, B, n_tokens, max_len);
-  const size_t need = workspace_bytes_of(pool, B, split_of(pool, B, 0, max_len));
+  const size_t need = workspace_bytes_of(pool, B, split_of(pool, B, max_len, max_len));
   if (need > 0 && (!workspace || workspace_bytes < need ||
                    reinterpret_cast<uintptr_t>(workspace) % 16 != 0))
     return fail(DAMP_ERR_INVALID_ARG, "%s: needs %zu bytes of 16-byte aligned workspace", name,

@@ -101,6 +101,25 @@ def test_linear_refusals(L):
         assert st == D.DAMP_ERR_UNSUPPORTED
 
 
+def test_prefill_workspace_holds_what_a_call_may_cut(L):
+    """The state of each piece of a request, with its decay: one long request
+    is cut into as many pieces as fill the device and not more, and short or
+    many requests need nothing."""
+    pool = pool_of(dk=128, dv=128, layers=1, slots=2, hv=32)
+    need = lambda B, n: L.damp_linear_prefill_workspace_bytes(ctypes.byref(pool), B, n)  # noqa: E731
+    piece = 32 * (128 * 128 * 4 + 8)
+    assert need(1, 32768) == 16 * piece  # 16 x 32 heads: two workgroups a CU
+    assert need(1, 1 << 20) == 16 * piece
+    assert need(1, 512) == 4 * piece and need(1, 257) == 3 * piece
+    assert need(1, 256) == 0 and need(1, 0) == 0 and need(512, 4096) == 0
+    # refused with a byte less, whatever the number of tokens
+    for n_tokens in (1000, 5000):
+        args = [ctypes.byref(pool), 0, P, None, 1, n_tokens, 1000, P, P, 4, P, 512, P, 512, P, 4096,
+                P, 32, 1.0, P, D.DAMP_DT_FP32, P, need(1, 1000) - 1, None]
+        st, msg = status(L.damp_linear_prefill, *args)
+        assert st == D.DAMP_ERR_INVALID_ARG and "workspace" in msg
+
+
 def test_verify_refusals(L):
     need = L.damp_verify_workspace_bytes(4, 1000)
     assert need > 0
