@@ -9,6 +9,8 @@ FP32 = 2e-6 leaves a factor of three, and is under what operands cut to 16
 bits in two parts would leave (2.8e-6). A bf16 output is off by at most half a
 step beside that: bf16 has 8 significant bits, so 2^-8 of its value.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -480,6 +482,95 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((o, o1, x.now), want[i])), i
         torch.randn(1000, device="cuda").sum().item()
+
+
+def check_states(x, slot_in, slot_out, starts, lens):
+    """Every written state by its own norm, every other one to the bit."""
+    slots, written = x.state.shape[0], set()
+    for b, (a, c) in enumerate(zip(slot_in, slot_out)):
+        if -1 <= a < slots and 0 <= c < slots:
+            _, S1 = x.want(starts[b], lens[b], a)
+            written.add(c)
+            for h in range(x.HV):
+                assert rel(x.now[c, h], S1[h]) <= FP32, (b, h)
+    rest = [s for s in range(slots) if s not in written]
+    assert torch.equal(x.now[rest].cpu(), x.state[rest])
+
+
+@pytest.mark.parametrize("HV,HK,dk,dv", [(32, 16, 128, 128), (32, 32, 128, 64), (16, 1, 256, 256),
+                                         (24, 8, 64, 128)])
+@pytest.mark.parametrize("o_type", [torch.float32, torch.bfloat16])
+def test_prompt_heads_of_a_model(HV, HK, dk, dv, o_type):
+    """As many heads as models have: several workgroups of a head, heads that
+    share keys in the order of the XCDs, whole and cut into segments; the same
+    bits on every run."""
+    print(f"prompt heads {HV} {HK} {dk}x{dv} {o_type}", flush=True)
+    for seed, lens in ((60, [300, 2, 65]), (61, [33] * 5)):
+        B = len(lens)
+        x = Setup(seed, sum(lens), HV, HK, dk, dv, 2 * B, fused=True)
+        starts = np.concatenate([[0], np.cumsum(lens)[:-1]])
+        slot_in, slot_out = list(range(B)), list(range(B, 2 * B))
+        o = run_prompts(x, lens, slot_in, slot_out, o_type=o_type)
+        check_states(x, slot_in, slot_out, starts, lens)
+        state = x.now.clone()
+        again = run_prompts(x, lens, slot_in, slot_out, o_type=o_type)
+        assert torch.equal(o, again) and torch.equal(state, x.now)
+
+
+@pytest.mark.parametrize("T,HV,dk,dv", [(1, 3, 128, 128), (1, 2, 64, 64), (63, 3, 128, 128),
+                                        (65, 2, 256, 40), (200, 2, 16, 16)])
+def test_prompt_states_by_slot(T, HV, dk, dv):
+    """Small states in a pool of larger ones."""
+    print(f"prompt states {T} {HV} {dk}x{dv}", flush=True)
+    x = Setup(62 + T, 2 * T, HV, 1, dk, dv, 7)
+    slot_in, slot_out = [-1, 4], [5, 4]
+    run_prompts(x, [T, T], slot_in, slot_out)
+    check_states(x, slot_in, slot_out, [0, T], [T, T])
+
+
+@pytest.mark.parametrize("o_type", [torch.float32, torch.bfloat16])
+def test_prompt_slots_in_segments(o_type):
+    """Padded requests, states that are not kept, one state continued by several
+    requests and a copy by a request of length 0, in a call whose requests are
+    cut into segments."""
+    print(f"prompt slots in segments {o_type}", flush=True)
+    lens = [700, 300, 513, 400, 1, 600, 0, 129]
+    starts = np.concatenate([[0], np.cumsum(lens)[:-1]])
+    x = Setup(70, sum(lens), 2, 1, 64, 64, 12)
+    assert S.damp_linear_prefill_workspace_bytes(x.pool, len(lens), max(lens)) > 0
+    slot_in, slot_out = [3, 3, -5, 12, 3, -1, 3, 0], [4, -1, 6, 7, 8, -1, 9, 0]
+    run_prompts(x, lens, slot_in, slot_out, o_type=o_type)
+    check_states(x, slot_in, slot_out, starts, lens)
+
+
+def test_decays_in_wider_rows():
+    """g_stride above HV: decays left in a wider row of a projection."""
+    print("g stride", flush=True)
+    n, HV = 333, 3
+    x = Setup(71, n, HV, 1, 64, 64, 4)
+    wide = torch.full((n, 11), float("nan"), device="cuda")
+    wide[:, 4:4 + HV] = x.g.cuda()
+    g = wide[:, 4:]
+    q, k, v = x.dev
+    o, ws = torch.empty(n, HV, 64, device="cuda"), torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    at = lambda t: t.data_ptr()  # noqa: E731
+    ids, into, start, lens = i32([1]), i32([2]), i32([0]), i32([n])
+    operands = [1, at(q), 64, at(k), 64, at(v), 64 * HV, at(g), 11, x.scale, at(o), D.DAMP_DT_FP32]
+    stream = torch.cuda.current_stream().cuda_stream
+    assert S.damp_linear_prefill_workspace_bytes(x.pool, 1, n) <= ws.numel()
+    D._check(S.lib().damp_linear_prefill(ctypes.byref(x.pool.desc), 0, at(ids), at(into), 1, n, n,
+                                         at(start), at(lens), *operands, at(ws), ws.numel(), stream))
+    w, S1 = x.want(0, n, 1)
+    check_o(o, w)
+    assert rel(x.now[2], S1) <= FP32
+    x.now.copy_(x.state)
+    slots = i32([0, 1, 2])
+    D._check(S.lib().damp_linear_update(ctypes.byref(x.pool.desc), 0, at(slots), None, 3, *operands,
+                                        stream))
+    for b in range(3):
+        w, S1 = x.want(b, 1, b)
+        check_o(o[b], w[0])
+        assert rel(x.now[b], S1) <= FP32
 
 
 def test_a_stream_of_the_callers_with_the_bindings_scratch():

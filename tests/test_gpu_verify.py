@@ -66,6 +66,25 @@ def test_the_largest_batch():
     assert torch.equal(o[:, 0].long(), at) and not bool(a.any())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_requests_of_several_workgroups(dtype):
+    """Batches whose requests are each summed by several workgroups, one
+    workspace for all of them: the last workgroup of each is found, whichever
+    it is, call after call."""
+    print(f"verify several workgroups {dtype}", flush=True)
+    piece = 256 if dtype is torch.float32 else 512
+    # pieces of a row, and workgroups of 4 waves that take ceil(pieces B / 4096) each
+    shapes = [(700, 13, 2), (128, 9, 3), (500, 21, 2), (40, 33, 9), (3, 64, 16)]
+    ws = torch.zeros(max(S.damp_verify_workspace_bytes(B, piece * n) for B, n, _ in shapes),
+                     dtype=torch.uint8, device="cuda")
+    for B, n, blocks in shapes:
+        steps = -(-n * B // 4096)
+        assert -(-n // (4 * steps)) == blocks
+        for seed in range(3):
+            check(*case(B + seed, B, 1, piece * n - 5 * seed, dtype), ws=ws)
+        assert not bool(ws[:1 << 18].any())
+
+
 def test_lengths():
     """Drafts of every length beside each other; lengths are cut to [0, K]."""
     print("verify lengths", flush=True)
