@@ -2,8 +2,11 @@
 refusals. No GPU needed: every call fails validation or has nothing to do."""
 import contextlib
 import ctypes
+import glob
 import os
 import re
+import shutil
+import subprocess
 import types
 
 import numpy as np
@@ -161,6 +164,74 @@ def test_slots_refusals(L):
         a = list(comp)
         a[i] = val
         assert L.damp_slots_compact(*a) == D.DAMP_ERR_INVALID_ARG, (i, val)
+
+
+# ------------------------------------------------------------ the built code
+
+OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
+
+
+def chunk_loops(listing):
+    """{kernel: instructions of its outermost loops with matrix products} of the
+    prompt kernels in a disassembly."""
+    loops, name, code = {}, None, []
+
+    def close():
+        if name is None or "prompt_chunks" not in name:
+            return
+        at = {addr: i for i, (addr, _) in enumerate(code)}
+        base, spans = code[0][0], []
+        for i, (_, text) in enumerate(code):
+            to = re.search(r"^s_c?branch\S* .*<\S+?(?:\+0x([0-9a-f]+))?>$", text)
+            if to and at[base + int(to.group(1) or "0", 16)] <= i:
+                spans.append((at[base + int(to.group(1) or "0", 16)], i))
+        spans = [(a, b) for a, b in spans if any("v_mfma" in t for _, t in code[a:b + 1])]
+        loops[name] = [t for i, (_, t) in enumerate(code) if any(a <= i <= b for a, b in spans)]
+
+    for line in listing.splitlines():
+        head = re.match(r"[0-9a-f]+ <(\S+)>:$", line)
+        if head:
+            close()
+            name, code = head.group(1), []
+        elif name and "//" in line:
+            text, addr = line.split("//", 1)
+            where = addr.split(":", 1)
+            target = re.search(r"<\S+>", where[1])
+            code.append((int(where[0], 16), text.strip() + (" " + target.group(0) if target else "")))
+    close()
+    return loops
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="no disassembler")
+def test_chunk_loops_have_no_branch_by_the_mask(L, tmp_path):
+    """In a branch that only some lanes take, a register saved at its head's
+    join is lost to the others: seen in a build of the prompt kernel whose
+    registers were short. Its chunk loops hold none, in any of its forms."""
+    lib = shutil.copy(D.LIB_PATH, tmp_path)
+    subprocess.run([OBJDUMP, "--offloading", lib], check=True, capture_output=True)
+    loops = {}
+    for f in glob.glob(lib + ".*gfx950"):
+        code = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", f], check=True,
+                              capture_output=True, text=True).stdout
+        loops.update(chunk_loops(code))
+    assert len(loops) == 18  # d_k to 64, 128, 256; two and four waves; three sets of parts
+    for name, code in loops.items():
+        assert sum("v_mfma" in t for t in code) >= 24, name
+        assert not [t for t in code if "saveexec" in t or "s_cbranch_execz" in t], name
+
+
+def test_the_reader_of_loops_sees_a_branch_by_the_mask():
+    listing = """
+0000000000001000 <a_prompt_chunks_a>:
+\ts_mov_b32 s0, 0   // 000000001000:
+\tv_mfma_f32_32x32x16_bf16 v[0:15], v[0:3], v[4:7], v[0:15]   // 000000001004:
+\ts_and_saveexec_b64 s[0:1], vcc   // 00000000100C:
+\ts_cbranch_scc1 65532   // 000000001010: <a_prompt_chunks_a+0x4>
+\ts_endpgm   // 000000001014:
+"""
+    loops = chunk_loops(listing)
+    assert [t.split()[0] for t in loops["a_prompt_chunks_a"]] == [
+        "v_mfma_f32_32x32x16_bf16", "s_and_saveexec_b64", "s_cbranch_scc1"]
 
 
 # ------------------------------------------------ what the binding allocates
