@@ -398,11 +398,12 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
     for (int i = 0; i < kLoads; ++i) load(head, i);
     if (decays) {
       load_g(0);
-      load_g(scan_g(0));
+      scan_g(0);
     }
     stage();
     __syncthreads();  // the first chunk is there
     n = __builtin_amdgcn_readfirstlane(chunk_len[0]);
+    if (decays) load_g(n);
     // (past the end the buffers are empty and their loads give zeros)
     const Rows next = rows(n);
 #pragma unroll
@@ -582,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, DK <= 128 ? 2 : 1) void prompt_chunks(cons
         }
       }
     }
-    __syncthreads();  // the next chunk is there
+    if (more) __syncthreads();  // the next chunk is there
   }
 
   // ---- the state after the last token
