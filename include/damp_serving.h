@@ -40,7 +40,8 @@ extern "C" {
  * with g_t one fp32 number per token and head (a log-decay; 0 keeps the
  * state, -inf forgets it, up to 88, whose factor fp32 just holds, grows it).
  * Over any number of tokens that grow, results are the recurrence's as long as
- * its own states and outputs stay in fp32. The states live in a DAMP_STATE_FP32 pool with
+ * its own states and outputs stay in fp32 (prompts: states, |v_t| and
+ * |q_t . k_j| below 2^111). The states live in a DAMP_STATE_FP32 pool with
  * d_k and d_v multiples of 8 up to 256, not necessarily equal. Other pools
  * return DAMP_ERR_UNSUPPORTED.
  *
@@ -64,6 +65,11 @@ extern "C" {
  * may reach any output of its own request, those of earlier tokens included,
  * and its state; it reaches no other request, and what lies outside the
  * requests' tokens is not read.
+ * States, and outputs in fp32, are good to fp32. For outputs in bf16 a prompt's
+ * fp32 intermediates (the state, the decayed scores and values) enter the
+ * products with 16 bits: an output may be off by 2^-15 of the sum of its terms'
+ * absolute values, beside its own rounding of up to 2^-8. That shows where the
+ * terms nearly cancel; callers who need those outputs take o in fp32.
  * o [tokens, HV, d_v] contiguous in o_dtype (DAMP_DT_FP32 or DAMP_DT_BF16),
  * 16-byte aligned.
  * ---------------------------------------------------------------------- */

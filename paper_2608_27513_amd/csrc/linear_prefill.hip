@@ -22,7 +22,8 @@
 // q, k, v are bf16 and enter as they are. What is fp32 (S, P, D V) enters as
 // a sum of bf16 parts, x = x1 + x2 (+ x3), each the rounding of what the
 // parts before it leave: three parts hold all 24 bits (the state, and o in
-// fp32), two hold 16 (for o in bf16, whose own rounding is 2^-8).
+// fp32), two hold 16 (for o in bf16, whose own rounding is 2^-8: with three, 423
+// us against 368 at 32768 tokens, 164 against 150 for eleven packed prompts).
 //
 // Log-decays are summed in double, in units of log2: their differences stay
 // good to fp32 however far the sum has run. A log-decay below -1000 counts as
@@ -35,10 +36,10 @@
 // q, k, v and o set the floor: memory, as 4 d_k d_v operations a token and head
 // are few beside their bytes. What bounds the kernel is the issue of vector and matrix
 // instructions and the waits between them: at 32768 tokens, 32 heads of 128 and
-// o in bf16, 376 us in three launches (128 + 12 + 237 at their fastest in a
-// profile, 137 + 12 + 252 at the median there), 183 TFLOP/s of the recurrence's
+// o in bf16, 372 us in three launches (130 + 11 + 235 at their fastest in a
+// profile, 136 + 12 + 245 at the median there), 185 TFLOP/s of the recurrence's
 // operations and 2.2 TB/s of the floor's bytes, the third launch with its matrix
-// units busy 36% and its vector issue 40% of the time, two waves a SIMD. Tried
+// units busy 37% and its vector issue 41% of the time, 1.6 waves a SIMD. Tried
 // and not kept: the parts of the next step placed between the products of this
 // one (the same time), a fourth wave that repeats a score tile to avoid the
 // branch (slower).
@@ -650,10 +651,11 @@ __global__ __launch_bounds__(256) void prompt_states(const PromptParams pp) {
 // request of up to kUncut is not cut: the two other launches would cost more),
 // and no shorter than the finest cut, which goes by B and max_len alone. More
 // tokens never make shorter segments, so the workspace for n_tokens = max_len,
-// the least there can be, has room for all of a B and max_len. Measured on 256 CUs, in us: one request of
-// 32768 tokens and 32 heads in 512 / 1024 / 2048 / 4096 pieces 391 / 416 / 444
-// / 522; eleven of 1 to 4096 tokens in 240 / 490 / 970: 214 / 155 / 157; one
-// of 200 whole 22, in two 27; one of 500 in segments of 128 / 256: 30 / 40.
+// the least there can be, has room for all of a B and max_len. Measured on 256
+// CUs, in us, with kWorkgroups = 512 / 1024 / 2048 / 4096: one request of 32768
+// tokens and 32 heads 373 / 389 / 418 / 465; eleven of 0 to 4096 tokens 152 /
+// 150 / 184 / 185; sixteen of 2000 and 64 columns 151 / 175 / 185 / 203. One of
+// 200 tokens whole 19, in two 25; one of 500 in segments of 128 / 256: 27 / 37.
 constexpr int kWorkgroups = 512;
 constexpr int kMostWorkgroups = 4096;
 constexpr int kLeastSegment = 128, kUncut = 256;
@@ -697,8 +699,8 @@ void launch(const PromptParams& p, int B, hipStream_t s) {
 }
 
 // Two waves where the head has no columns for four: 16 requests of 2000 tokens,
-// 32 heads of 64, take 165 us against 170, with keys of 128 channels 195 against
-// 214.
+// 32 heads of 64, take 151 us against 155, with keys of 128 channels 194 against
+// 218.
 template <int DK>
 void launch(const PromptParams& p, int B, hipStream_t s) {
   if (p.l.dv <= 64) launch<DK, 2>(p, B, s);

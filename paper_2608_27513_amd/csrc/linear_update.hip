@@ -216,10 +216,10 @@ void launch(const LinearParams& p, int B, hipStream_t s) {
 
 // Fewer tiles than CUs: 32 columns each, for the shorter chain of loads (one
 // request of 32 heads: 3.4 us against 4.0 with 128). Otherwise the whole row,
-// up to 128 columns. States of 128 MB and more pass by the caches (256
-// requests: 196 against 211 us; 64 requests, 134 MB: 50.9 against 53.5);
-// smaller ones may still be there from the step before (32 requests: 21.7 us
-// against 26.6).
+// up to 128 columns. States of 128 MB and more whose rows are wider than 32
+// columns pass by the caches (256 requests: 196 against 211 us; 64 requests, 134
+// MB: 50.9 against 53.5); smaller ones may still be there from the step before
+// (32 requests: 21.7 us against 26.6).
 constexpr int64_t kFewTiles = 256;
 constexpr int64_t kStreamBytes = int64_t{128} << 20;
 

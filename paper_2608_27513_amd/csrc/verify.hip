@@ -1,6 +1,9 @@
 // Verification of drafted tokens (damp_serving.h): which drafts stand, and
 // the next token drawn from what the target has over the draft.
 //
+// The scheme is the published rejection sampling of speculative decoding
+// (Leviathan, Kalman and Matias, 2023; Chen et al., 2023), decided exactly.
+//
 // One row of V weights is summed and searched for each request (its first
 // refused draft's, or the one after its last), so the row's bytes, of p and
 // after a refusal of q, bound the operator; short rows are bound by the chain

@@ -295,8 +295,8 @@ def test_prompt_decays():
 
 def check_terms(x, o, start, length, slot):
     """bf16 outputs of one request: half a step of bf16, and of the sum of the
-    terms' absolute values 2^-18 for the state's and 2^-18 for the scores' two
-    bf16 parts (each leaves 2^-9 of what it is rounded from), and fp32's."""
+    terms' absolute values 2^-17 and fp32's. (Two bf16 parts leave at most 2^-16
+    of a term; not of every term, nor with one sign.)"""
     q, k, v = (t[start:start + length].abs() for t in x.cpu)
     S0 = x.state[slot].abs() if slot >= 0 else torch.zeros_like(x.state[0])
     terms, _ = ref.linear(q, k, v, x.g[start:start + length], S0, x.scale)
